@@ -406,6 +406,127 @@ prq_status prq_forward_host(const prq_weights *w, prq_act_mode mode, const uint1
                             void *y_host, prq_dtype y_dtype, void *dev_scratch, size_t scratch_bytes,
                             prq_stream_t stream);
 
+/* ---- beside the projections ---------------------------------------------------------------- */
+
+/* Low-rank adapters of many requests beside one shared projection.  (Not in the paper.)  The quantised weights of a layer
+ * serve every request of a batch, so an adapter cannot be merged into them; its product is added to the layer's output:
+ *   y[m, n] = base[m, n] + scale[a] * sum_{r < rank[a]} (sum_k x[m, k] A[a][p][r][k]) * B[a][n][r],    a = row_adapter[m],
+ * p the part that column n lies in.  Parts are the layers of a stacked projection (q / k / v, gate / up): they read the same x, and
+ * each has its own A.  One pool holds the adapters of all requests, a program writes an adapter's matrices into a free slot.
+ * The sums are held in fp32; the low-rank product in between is kept to 16 bits or more of significand, y is rounded once.  */
+#define PRQ_ADAPTER_MAX_RANK 128
+typedef struct prq_adapters {
+    size_t struct_size;          /* sizeof(prq_adapters)                                                         */
+    int n_slots;                 /* adapters that the pool has room for, >= 1                                    */
+    int max_rank;                /* rows of A and columns of B kept per part: a multiple of 8, 8 .. PRQ_ADAPTER_MAX_RANK */
+    int K;                       /* input channels of the projection, K % 32 == 0                                */
+    int n_parts;                 /* 1 .. PRQ_MULTI_MAX                                                           */
+    int part_N[4];               /* output features of each part; multiples of 8 but for the last one; N is their sum */
+    const void *A;               /* device, n_slots x n_parts x max_rank x K bf16, 16-byte aligned               */
+    const void *B;               /* device, n_slots x N x max_rank bf16, 16-byte aligned                         */
+    const float *scale;          /* device, n_slots factors; NULL: 1                                             */
+    const int32_t *ranks;        /* device, n_slots ranks, taken into [0, max_rank]; NULL: max_rank.  What A and B hold beyond an
+                                    adapter's rank is not used (it may be anything, NaN among it)                */
+} prq_adapters;
+
+/* Scratch of one prq_linear_adapters call for M rows; it need not be cleared, and calls that may overlap need one each.
+ * Returns 0 for invalid arguments, and where none is needed. */
+size_t prq_adapters_workspace_bytes(const prq_adapters *a, int M);
+
+/*   row_adapter  device, M int32: each row's slot.  A row whose entry is not in [0, n_slots) -- -1, say -- has no adapter.  Rows
+ *                of one adapter need not follow one another.
+ *   x            device, M x K bf16, row stride ldx elements (multiple of 8), 16-byte aligned: the activation as A expects it.
+ *                For a layer in PRQ_ACT_IDENTITY mode, whose producer emits scaled and permuted channels, fold A with
+ *                prq_fold_adapter.
+ *   base         device, M x N, row stride ldbase, dtype y_dtype: the projection's output
+ *   y            device out, M x N, row stride ldy, same type; may be `base` itself (with ldy == ldbase), must not overlap it
+ *                otherwise.  Rows without an adapter get base's values (bit for bit; in place they are not touched), and
+ *                so do rows whose adapter has rank 0.
+ *   workspace    device, prq_adapters_workspace_bytes(a, M) bytes, 16-byte aligned
+ * Both matrices 16-byte aligned, their strides multiples of 8 (bf16) or 4 (fp32) elements.  Buffers belong to the current device.
+ * The kernels read row_adapter, ranks, scale, A and B when they run: a captured call follows what a program writes there.
+ * A value that is not finite in x, or in an adapter, reaches the rows of that row's, of that adapter's requests only.
+ * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, UNSUPPORTED_ARCH, CUDA.  M == 0 is a no-op. */
+prq_status prq_linear_adapters(const prq_adapters *a, const int32_t *row_adapter, const void *x, int M, int ldx, const void *base,
+                               int ldbase, void *y, int ldy, prq_dtype y_dtype, void *workspace, size_t workspace_bytes,
+                               prq_stream_t stream);
+
+/* The counterpart of prq_fold_producer for an adapter's A: for activations Z D^-1 P
+ *   out[r, j] = bf16( A[r, perm[j]] * s[perm[j]] )     (exact product, rounded once, ties to even)
+ * All pointers are HOST memory: perm and s K entries each, as prq_weights_get returns them (PRQ_FIELD_PERM, PRQ_FIELD_S); A, out
+ * rows x K bf16.  INVALID_ARG for a perm entry outside [0, K) and an s that is not finite. */
+prq_status prq_fold_adapter(const int32_t *perm, const float *s, int K, const uint16_t *A, int rows, uint16_t *out);
+
+/* Position rotation of the projections' heads.  (Not in the paper.)  Pair i of a head turns by the angle position * f_i:
+ *   (a, b) -> factor * (a cos - b sin, b cos + a sin),
+ * i in [0, rot_dim / 2).  A handle holds the frequencies f_i, worked out in FP64, as fractions of a turn in 64-bit fixed point: a kernel
+ * multiplies them by the position exactly, modulo whole turns, so that the angle is as exact at position 2^31 as at 1, and no
+ * table of angles exists. */
+typedef struct prq_rope prq_rope;
+typedef enum {
+    PRQ_ROPE_HALF = 0,         /* pair i is elements i and i + rot_dim / 2 */
+    PRQ_ROPE_INTERLEAVED = 1   /* pair i is elements 2 i and 2 i + 1       */
+} prq_rope_layout;
+typedef enum {
+    PRQ_ROPE_UNSCALED = 0,     /* f_i = base^(-2 i / rot_dim)                                                          */
+    PRQ_ROPE_LINEAR = 1,       /* f_i / factor                                                                         */
+    PRQ_ROPE_BASE = 2,         /* base * factor^(rot_dim / (rot_dim - 2)) in the place of base (rot_dim > 2)           */
+    PRQ_ROPE_YARN = 3,         /* YaRN (Peng et al., 2023): from f_i to f_i / factor along a ramp over i, between the pairs that make
+                                  beta_fast and beta_slow turns over original_positions (floor and ceiling of their indices, within
+                                  [0, rot_dim - 1]); the result is multiplied by 0.1 ln(factor) + 1                     */
+    PRQ_ROPE_WAVELENGTH = 4    /* from f_i to f_i / factor linearly in the turns t_i = original_positions f_i / 2 pi: f_i where
+                                  t_i >= high_factor, f_i / factor where t_i <= low_factor                             */
+} prq_rope_scaling;
+/* Set struct_size = sizeof(prq_rope_opts).  Zero means the default in brackets; fields that a scaling does not use are not read. */
+typedef struct prq_rope_opts {
+    size_t struct_size;
+    int head_dim;              /* 2 .. 512                                                     */
+    int rot_dim;               /* the first elements of a head turn; even, 2 .. min(head_dim, 256) [head_dim] */
+    int layout;                /* a prq_rope_layout                                            */
+    int scaling;               /* a prq_rope_scaling                                           */
+    int original_positions;    /* YARN, WAVELENGTH                                             */
+    double base;               /* > 1 [10000]                                                  */
+    double factor;             /* >= 1 [1]                                                     */
+    double beta_fast;          /* YARN [32]                                                    */
+    double beta_slow;          /* YARN [1]                                                     */
+    double low_factor;         /* WAVELENGTH [1]                                               */
+    double high_factor;        /* WAVELENGTH, > low_factor [4]                                 */
+    double attention_factor;   /* what rotated elements are multiplied by [YARN as above, otherwise 1] */
+} prq_rope_opts;
+
+/* Host only: a handle belongs to no device, is immutable, and may be used by several threads and streams. */
+prq_status prq_rope_create(const prq_rope_opts *opts, prq_rope **out);
+void prq_rope_free(prq_rope *r);   /* a null handle is a no-op; work in flight is not disturbed */
+/* The frequencies (rot_dim / 2 doubles, host) and the factor of a handle, for checks and export.  Either may be NULL. */
+prq_status prq_rope_frequencies(const prq_rope *r, double *f, double *attention_factor);
+
+/* The heads of M rows of one tensor: element j of head h of row m stands at x[m * ldx + h * hsx + j], and its result goes to
+ * out[m * ldout + h * hsout + j].  Strides in elements.  `out` may be `x` (with the same strides); otherwise the two must not overlap,
+ * nor may heads overlap one another.  A head's elements follow one another; everything else may have any stride and alignment (16-byte
+ * aligned pointers and strides, and rot_dim and head_dim multiples of 16, take the fast kernel). */
+typedef struct prq_heads {
+    const void *x;             /* device */
+    void *out;                 /* device */
+    int64_t ldx, hsx, ldout, hsout;
+    int heads;                 /* 0: nothing (then x and out may be NULL) */
+    const float *weight;       /* device, head_dim factors of the norm, NULL: 1.  Not used by prq_rotate_heads */
+} prq_heads;
+
+/* Rotates the query and the key heads (k may be NULL) of M rows in one launch: of q / k / v as the stacked projection left them side by
+ * side, of separate matrices, of keys on their way into a cache.
+ *   positions  device, M int32.  A negative position turns the other way: that moves keys which were rotated already, and (the
+ *              rotation's transpose) takes gradients back.  Rows at PRQ_POSITION_NONE are left out: their outputs stay as they are.
+ *   dtype      of both tensors.  Rotations are worked out in fp32 and rounded once.
+ * Errors: INVALID_ARG, ALIGNMENT (pointers not aligned to an element), UNSUPPORTED_ARCH, CUDA.  M == 0 is a no-op. */
+#define PRQ_POSITION_NONE INT32_MIN
+prq_status prq_rotate_heads(const prq_rope *r, const int32_t *positions, int M, const prq_heads *q, const prq_heads *k, prq_dtype dtype,
+                            prq_stream_t stream);
+
+/* The same with the RMS norm of every head in front, in one pass over the data: z = x / sqrt(mean(x^2) + eps) * weight over the
+ * whole head, in fp32, then the rotation of z.  eps > 0. */
+prq_status prq_norm_rotate_heads(const prq_rope *r, const int32_t *positions, int M, const prq_heads *q, const prq_heads *k, float eps,
+                                 prq_dtype dtype, prq_stream_t stream);
+
 /* ---- diagnostics ----------------------------------------------------------------------- */
 
 const char *prq_status_string(prq_status s);

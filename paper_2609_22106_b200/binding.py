@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import numpy as np
 
@@ -29,6 +30,8 @@ EXPORTS = [
     "prq_status_string", "prq_last_device_status", "prq_kernel_launch_count", "prq_mxf4_peak_probe",
     "prq_handover_probe", "prq_stack_gate_up", "prq_linear_gated", "prq_weights_format", "prq_act_bytes_for",
     "prq_prepare_weights_stacked", "prq_linear_workspace_clear_bytes", "prq_release_cached_memory",
+    "prq_adapters_workspace_bytes", "prq_linear_adapters", "prq_fold_adapter", "prq_rope_create", "prq_rope_free", "prq_rope_frequencies",
+    "prq_rotate_heads", "prq_norm_rotate_heads",
 ]
 
 
@@ -92,6 +95,16 @@ def lib():
         L.prq_act_bytes_for.restype = cs
         L.prq_stack_gate_up.argtypes = [vp, vp, ci, ci, vp]
         L.prq_linear_gated.argtypes = [vp, vp, vp, ci, vp, vp, vp, vp, vp, vp]
+        L.prq_adapters_workspace_bytes.argtypes = [vp, ci]
+        L.prq_adapters_workspace_bytes.restype = cs
+        L.prq_linear_adapters.argtypes = [vp, vp, vp, ci, ci, vp, ci, vp, ci, ci, vp, cs, vp]
+        L.prq_fold_adapter.argtypes = [vp, vp, ci, vp, ci, vp]
+        L.prq_rope_create.argtypes = [vp, ctypes.POINTER(vp)]
+        L.prq_rope_free.argtypes = [vp]
+        L.prq_rope_free.restype = None
+        L.prq_rope_frequencies.argtypes = [vp, vp, vp]
+        L.prq_rotate_heads.argtypes = [vp, vp, ci, vp, vp, ci, vp]
+        L.prq_norm_rotate_heads.argtypes = [vp, vp, ci, vp, vp, cf, ci, vp]
         _lib = L
     return _lib
 
@@ -524,3 +537,178 @@ def prepare_weights_stacked(Ws, act_amax: np.ndarray, alpha: float, k_tail: int,
                                              _np_ptr(amax), alpha, k_tail, ctypes.cast(ctypes.pointer(o), ctypes.c_void_p),
                                              ctypes.byref(h)), "prq_prepare_weights_stacked")
     return Weights(h)
+
+
+def _require(ok: bool, where: str):
+    """What the C call cannot see of a tensor (its type, its device, the stride of its last dimension) is checked here."""
+    if not ok:
+        raise PrqError(1, where)
+
+
+_current_device = None
+
+
+def _on_current_device(*tensors) -> bool:
+    global _current_device
+    if _current_device is None:
+        import torch
+
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    dev = _current_device()
+    return all(t is None or t.get_device() == dev for t in tensors)
+
+
+ADAPTER_MAX_RANK = 128
+
+
+class AdapterPool(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_size_t), ("n_slots", ctypes.c_int), ("max_rank", ctypes.c_int), ("K", ctypes.c_int), ("n_parts", ctypes.c_int),
+                ("part_N", ctypes.c_int * 4), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("ranks", ctypes.c_void_p)]
+
+
+class Adapters:
+    """A pool of low-rank adapters of one (plain or stacked) projection.  A: bf16 CUDA tensor (slots, parts, max_rank, K), or (slots, max_rank,
+    K) for one part; B: (slots, N, max_rank); parts: output features of each part; scale: fp32 (slots,) or None; ranks: int32 (slots,) or
+    None.  The tensors are kept and read by every call: write an adapter into a free slot of them."""
+
+    def __init__(self, A, B, parts, scale=None, ranks=None):
+        import torch
+
+        A = A if A.dim() == 4 else A[:, None]
+        parts = [int(n) for n in parts]
+        S, P, R, K = A.shape
+        where = "Adapters"
+        _require(A.dtype == B.dtype == torch.bfloat16 and A.is_contiguous() and B.is_contiguous(), where)
+        _require(1 <= len(parts) <= MULTI_MAX and P == len(parts) and tuple(B.shape) == (S, sum(parts), R), where)
+        for t, dtype in ((scale, torch.float32), (ranks, torch.int32)):
+            _require(t is None or (t.dtype == dtype and tuple(t.shape) == (S,) and t.is_contiguous()), where)
+        _require(all(t is None or t.get_device() == A.get_device() for t in (B, scale, ranks)) and A.is_cuda, where)
+        self.A, self.B, self.scale, self.ranks, self.parts, self.N, self.K = A, B, scale, ranks, parts, sum(parts), K
+        self._pool = AdapterPool(ctypes.sizeof(AdapterPool), S, R, K, P, (ctypes.c_int * 4)(*parts), _dptr(A), _dptr(B), _dptr(scale), _dptr(ranks))
+        self._p = ctypes.addressof(self._pool)
+
+
+def adapters_workspace(adapters: Adapters, M: int):
+    """Scratch for linear_adapters on up to M rows; calls that may overlap need one each."""
+    import torch
+
+    return torch.empty(max(int(lib().prq_adapters_workspace_bytes(adapters._p, M)), 16), dtype=torch.uint8, device=adapters.A.device)
+
+
+def linear_adapters(adapters: Adapters, x, row_adapter, base, out=None, workspace=None, stream=None):
+    """base + scale * (x A^T) B^T with the adapter that row_adapter (int32 (M,), -1: none) names for each row.  x: bf16 (M, K); base: the
+    projection's output, fp32 or bf16 (M, N).  Adds in place unless `out` is given; returns the result."""
+    import torch
+
+    M, out = x.shape[0], base if out is None else out
+    _require(x.dtype == torch.bfloat16 and row_adapter.dtype == torch.int32 and base.dtype == out.dtype and base.dtype in (torch.float32, torch.bfloat16) and
+             tuple(x.shape) == (M, adapters.K) and tuple(row_adapter.shape) == (M,) and tuple(base.shape) == tuple(out.shape) == (M, adapters.N), "linear_adapters")
+    if M == 0:
+        return out
+    _require((x.stride(1) == 1) and row_adapter.is_contiguous() and (adapters.N == 1 or base.stride(1) == out.stride(1) == 1) and
+             _on_current_device(x, row_adapter, base, out, workspace, adapters.A), "linear_adapters")
+    if workspace is None:
+        if stream is None:
+            workspace = adapters_workspace(adapters, M)
+        else:   # from the memory of the call's stream
+            with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=x.device)):
+                workspace = adapters_workspace(adapters, M)
+    one = M == 1   # a single row has no stride
+    _check(lib().prq_linear_adapters(adapters._p, _dptr(row_adapter), _dptr(x), M, adapters.K if one else x.stride(0), _dptr(base),
+                                     (adapters.N + 7) // 8 * 8 if one else base.stride(0), _dptr(out), (adapters.N + 7) // 8 * 8 if one else out.stride(0),
+                                     F32 if base.dtype == torch.float32 else BF16, _dptr(workspace), workspace.numel() * workspace.element_size(),
+                                     _stream_ptr(stream)), "prq_linear_adapters")
+    return out
+
+
+def fold_adapter(perm: np.ndarray, s: np.ndarray, A: np.ndarray) -> np.ndarray:
+    """An adapter's A (uint16 (rows, K)) for activations in a layer's permuted, scaled channel order (FIELD_PERM, FIELD_S): what ACT_IDENTITY
+    layers read."""
+    pm, sc, A = np.ascontiguousarray(perm, np.int32), np.ascontiguousarray(s, np.float32), np.ascontiguousarray(A, np.uint16)
+    out = np.empty_like(A)
+    _require(A.ndim == 2 and pm.shape == sc.shape == (A.shape[1],), "fold_adapter")
+    _check(lib().prq_fold_adapter(_np_ptr(pm), _np_ptr(sc), A.shape[1], _np_ptr(A), A.shape[0], _np_ptr(out)), "prq_fold_adapter")
+    return out
+
+
+class RopeOpts(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_size_t), ("head_dim", ctypes.c_int), ("rot_dim", ctypes.c_int), ("layout", ctypes.c_int), ("scaling", ctypes.c_int),
+                ("original_positions", ctypes.c_int), ("base", ctypes.c_double), ("factor", ctypes.c_double), ("beta_fast", ctypes.c_double),
+                ("beta_slow", ctypes.c_double), ("low_factor", ctypes.c_double), ("high_factor", ctypes.c_double), ("attention_factor", ctypes.c_double)]
+
+
+ROPE_LAYOUTS = {"half": 0, "pairs": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+POSITION_NONE = -2 ** 31
+
+
+class Rope:
+    """Frequencies of a position rotation (a prq_rope handle; see include/prq.h for the scalings: linear, ntk = by the base, yarn, bands = by
+    wavelength).  Zero takes a default."""
+
+    def __init__(self, head_dim: int, rot_dim: int = 0, layout: str = "half", scaling: str = "none", base: float = 0.0, factor: float = 0.0,
+                 original_positions: int = 0, beta_fast: float = 0.0, beta_slow: float = 0.0, low_factor: float = 0.0, high_factor: float = 0.0,
+                 attention_factor: float = 0.0):
+        self._h = None
+        _require(layout in ROPE_LAYOUTS and scaling in ROPE_SCALINGS, "Rope")
+        o = RopeOpts(ctypes.sizeof(RopeOpts), head_dim, rot_dim, ROPE_LAYOUTS[layout], ROPE_SCALINGS[scaling], original_positions, base, factor, beta_fast,
+                     beta_slow, low_factor, high_factor, attention_factor)
+        h = ctypes.c_void_p()
+        _check(lib().prq_rope_create(ctypes.addressof(o), ctypes.byref(h)), "prq_rope_create")
+        self._h, self.head_dim, self.rot_dim = h, head_dim, rot_dim or head_dim
+
+    def frequencies(self):
+        """(radians per position of every pair, the factor of rotated elements)"""
+        f, a = np.empty(self.rot_dim // 2, np.float64), ctypes.c_double()
+        _check(lib().prq_rope_frequencies(self._h, _np_ptr(f), ctypes.addressof(a)), "prq_rope_frequencies")
+        return f, a.value
+
+    def __del__(self):
+        try:
+            if self._h:
+                lib().prq_rope_free(self._h)
+                self._h = None
+        except Exception:
+            pass
+
+
+_HEADS = struct.Struct("@PPqqqqiP")   # prq_heads, in native alignment
+
+
+def _heads(t, to, weight, M: int, D: int, dtype, where: str):
+    """A prq_heads of a tensor (M, heads, D) and where its result goes."""
+    import torch
+
+    _require(t.dim() == 3 and t.shape[0] == M and t.shape[2] == D and t.shape == to.shape and t.dtype == to.dtype == dtype and
+             (D == 1 or (t.stride(2) == 1 and to.stride(2) == 1)) and _on_current_device(t, to, weight), where)
+    _require(weight is None or (weight.dtype == torch.float32 and tuple(weight.shape) == (D,) and weight.is_contiguous()), where)
+    sx, so = t.stride(), to.stride()
+    return _HEADS.pack(t.data_ptr(), to.data_ptr(), sx[0], sx[1], so[0], so[1], t.shape[1], 0 if weight is None else weight.data_ptr())
+
+
+def _rotate(rope, positions, q, k, weights, eps, out, stream, where):
+    import torch
+
+    to = ((q, k) if out is None else (out, None) if k is None else out)
+    M = positions.shape[0]
+    _require(positions.dtype == torch.int32 and positions.dim() == 1 and (M < 2 or positions.stride(0) == 1) and _on_current_device(positions) and
+             q.dtype in (torch.float32, torch.bfloat16), where)
+    hq = _heads(q, to[0], weights[0], M, rope.head_dim, q.dtype, where)
+    hk = None if k is None else _heads(k, to[1], weights[1], M, rope.head_dim, q.dtype, where)
+    dtype = F32 if q.dtype == torch.float32 else BF16
+    if eps is None:
+        _check(lib().prq_rotate_heads(rope._h, positions.data_ptr(), M, hq, hk, dtype, _stream_ptr(stream)), where)
+    else:
+        _check(lib().prq_norm_rotate_heads(rope._h, positions.data_ptr(), M, hq, hk, eps, dtype, _stream_ptr(stream)), where)
+    return to[0] if k is None else to
+
+
+def rotate_heads(rope: Rope, positions, q, k=None, out=None, stream=None):
+    """Turns the heads q (M, heads, head_dim) -- and k, in the same launch -- by their rows' positions (int32 (M,); POSITION_NONE: the row is
+    left out).  Tensors may be slices of the stacked projection's output.  In place unless out (a pair if k is given) is given."""
+    return _rotate(rope, positions, q, k, (None, None), None, out, stream, "prq_rotate_heads")
+
+
+def norm_rotate_heads(rope: Rope, positions, q, k=None, q_weight=None, k_weight=None, eps: float = 1e-6, out=None, stream=None):
+    """The RMS norm of every head (weights: fp32 (head_dim,) or None), then rotate_heads, in one pass."""
+    return _rotate(rope, positions, q, k, (q_weight, k_weight), eps, out, stream, "prq_norm_rotate_heads")

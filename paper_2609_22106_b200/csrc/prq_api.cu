@@ -482,6 +482,18 @@ size_t prefill_flag_bytes(const prq_weights* w, int M) {
 
 using namespace prq;
 
+namespace prq {
+prq_status current_device_ready(int* num_sms) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return PRQ_ERR_CUDA;
+    DeviceInfo* di;
+    const prq_status st = device_info(dev, &di);
+    if (st == PRQ_OK) *num_sms = di->num_sms;
+    return st;
+}
+void count_launches(int n) { g_launches.fetch_add(n); }
+}  // namespace prq
+
 extern "C" {
 
 const char* prq_status_string(prq_status s) {

@@ -142,6 +142,8 @@ prq_status prepare_layer_fp8(const uint16_t* W, int N, int K, const float* amax,
 // Gate and up projection rows interleaved in groups of 32 (rows 64 b .. 64 b + 31 = gate rows 32 b .., rows 64 b + 32 ..
 // 64 b + 63 = up rows 32 b ..): the layout prq_linear_gated expects.  Host buffers, C % 32 == 0.
 void stack_gate_up(const uint16_t* W_gate, const uint16_t* W_up, int C, int H, uint16_t* out);
+// An adapter's A for activations in a layer's permuted, scaled channel order: out[r, j] = bf16(A[r, perm[j]] * s[perm[j]]).  Host buffers.
+prq_status fold_adapter(const int32_t* perm, const float* s, int K, const uint16_t* A, int rows, uint16_t* out);
 // The heavy steps of the same on the GPU (prq_prep_device.cu), all experts of a layer per launch; device buffers.
 // Column errors of the scaled weights s: E x K, err: E x K doubles; *nonfinite becomes 1 if W * s holds a NaN or infinity.
 cudaError_t launch_col_err(const uint16_t* W, const float* s, int E, int N, int K, double* err, int* nonfinite, cudaStream_t stream);
@@ -153,7 +155,21 @@ struct SfLayout { uint8_t* dst; size_t bytes; int tile_rows, groups_per_tile, gr
 struct SfLayouts { int n, n_experts, group_bytes; SfLayout l[5]; };   // group_bytes: 1024, second format 512
 cudaError_t launch_sf_layout(const uint8_t* scales, int N, int K, int k_tail, const SfLayouts& t, int sm_count, cudaStream_t stream);
 
+// For entry points that take no handle (prq_api.cu): whether the current device can run the kernels, with its SM count; and the
+// library's count of its launches.
+prq_status current_device_ready(int* num_sms);
+void count_launches(int n);
+
 }  // namespace prq
+
+// Position rotation: frequencies, and the same as fractions of a turn in 64-bit fixed point.
+constexpr int kMaxPairs = 128;
+struct prq_rope {
+    int head_dim = 0, rot_dim = 0, layout = 0;
+    double attention_factor = 1.0;
+    double f[kMaxPairs] = {};
+    uint64_t turns[kMaxPairs] = {};
+};
 
 struct prq_weights {
     int n_experts = 0, N = 0, K = 0, k_tail = 0;

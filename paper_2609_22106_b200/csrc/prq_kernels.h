@@ -208,6 +208,42 @@ cudaError_t launch_prefill_pair_fp8(int bn, const CUtensorMap& tm_act, const CUt
 int prefill_pair_max_clusters(int bn);
 int prefill_pair_max_clusters_fp8();
 
+// Position rotation of heads, with or without the norm in front (prq_rope.cu).
+struct HeadRows {
+    const void* x;
+    void* out;
+    long long ldx, hsx, ldout, hsout;
+    int heads;
+    const float* weight;
+};
+struct RotateParams {
+    const int32_t* positions;
+    HeadRows t[2];               // queries, keys
+    int M;
+    int head_dim, rot_dim;
+    float eps, factor;
+    uint64_t turns[kMaxPairs];   // fraction of a turn per position, in 2^-64
+};
+cudaError_t launch_rotate_heads(const RotateParams& p, bool interleaved, bool norm, bool bf16, int num_sms, cudaStream_t stream);
+
+// Low-rank adapters beside a projection (prq_adapters.cu).
+struct AdapterParams {
+    const int32_t* row_adapter;
+    const uint16_t* x;
+    const void* base;
+    void* y;
+    const uint16_t* A;           // n_slots x n_parts x max_rank x K
+    const uint16_t* B;           // n_slots x N x max_rank
+    const float* scale;
+    const int32_t* ranks;
+    float* h;                    // M x n_parts x max_rank
+    long long ldx, ldbase, ldy;
+    int M, K, N, n_slots, max_rank, n_parts;
+    int part_end[kMaxBatch];     // column behind each part
+};
+size_t adapters_workspace_bytes(int M, int n_parts, int max_rank);
+cudaError_t launch_adapters(const AdapterParams& p, bool bf16, int num_sms, cudaStream_t stream, int* launches);
+
 // Benchmark utility: `grid` CTAs each issuing n_mma block-scaled FP4 MMAs (128 x 256 x 64) from shared memory.
 cudaError_t launch_mxf4_peak_probe(int n_mma, int grid, int* status, cudaStream_t stream);
 

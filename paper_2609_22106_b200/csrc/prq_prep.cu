@@ -158,6 +158,16 @@ prq_status fold_producer(const int32_t* perm, const float* inv_s, int C, int k_t
     return PRQ_OK;
 }
 
+prq_status fold_adapter(const int32_t* perm, const float* s, int K, const uint16_t* A, int rows, uint16_t* out) {
+    for (int j = 0; j < K; ++j)
+        if (perm[j] < 0 || perm[j] >= K || !std::isfinite(s[perm[j]])) return PRQ_ERR_INVALID_ARG;
+    parallel_for(rows, [&](long lo, long hi) {
+        for (long r = lo; r < hi; ++r)
+            for (int j = 0; j < K; ++j) out[r * K + j] = scaled_bf16(A[r * K + perm[j]], s[perm[j]]);
+    });
+    return PRQ_OK;
+}
+
 prq_status channel_scales(const float* amax, int K, float alpha, std::vector<float>& s, std::vector<float>& inv_s) {
     s.resize(K);
     inv_s.resize(K);
