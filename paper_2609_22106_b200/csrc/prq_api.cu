@@ -483,12 +483,15 @@ size_t prefill_flag_bytes(const prq_weights* w, int M) {
 using namespace prq;
 
 namespace prq {
-prq_status current_device_ready(int* num_sms) {
+prq_status current_device_ready(int* num_sms, int** status) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return PRQ_ERR_CUDA;
     DeviceInfo* di;
     const prq_status st = device_info(dev, &di);
-    if (st == PRQ_OK) *num_sms = di->num_sms;
+    if (st == PRQ_OK) {
+        *num_sms = di->num_sms;
+        *status = di->status_ptr;
+    }
     return st;
 }
 void count_launches(int n) { g_launches.fetch_add(n); }

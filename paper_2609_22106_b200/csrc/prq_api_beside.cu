@@ -70,7 +70,7 @@ prq_status rotate(const prq_rope* r, const int32_t* positions, int M, const prq_
     if (!positions) return PRQ_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(positions) % 4) return PRQ_ERR_ALIGNMENT;
     int sms = 0;
-    const prq_status st = current_device_ready(&sms);
+    const prq_status st = current_device_ready(&sms, &p.status);
     if (st != PRQ_OK) return st;
     p.positions = positions;
     p.M = M;
@@ -114,7 +114,7 @@ prq_status prq_linear_adapters(const prq_adapters* a, const int32_t* row_adapter
         if (!aligned16(workspace)) return PRQ_ERR_ALIGNMENT;
     }
     int sms = 0;
-    st = current_device_ready(&sms);
+    st = current_device_ready(&sms, &p.status);
     if (st != PRQ_OK) return st;
     p.row_adapter = row_adapter;
     p.x = static_cast<const uint16_t*>(x);

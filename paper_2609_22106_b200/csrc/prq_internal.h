@@ -155,9 +155,9 @@ struct SfLayout { uint8_t* dst; size_t bytes; int tile_rows, groups_per_tile, gr
 struct SfLayouts { int n, n_experts, group_bytes; SfLayout l[5]; };   // group_bytes: 1024, second format 512
 cudaError_t launch_sf_layout(const uint8_t* scales, int N, int K, int k_tail, const SfLayouts& t, int sm_count, cudaStream_t stream);
 
-// For entry points that take no handle (prq_api.cu): whether the current device can run the kernels, with its SM count; and the
+// For entry points that take no handle (prq_api.cu): whether the current device can run the kernels, with its SM count and status word; and the
 // library's count of its launches.
-prq_status current_device_ready(int* num_sms);
+prq_status current_device_ready(int* num_sms, int** status);
 void count_launches(int n);
 
 }  // namespace prq

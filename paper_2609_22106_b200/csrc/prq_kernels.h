@@ -222,6 +222,7 @@ struct RotateParams {
     int M;
     int head_dim, rot_dim;
     float eps, factor;
+    int* status;                 // device status word
     uint64_t turns[kMaxPairs];   // fraction of a turn per position, in 2^-64
 };
 cudaError_t launch_rotate_heads(const RotateParams& p, bool interleaved, bool norm, bool bf16, int num_sms, cudaStream_t stream);
@@ -237,6 +238,7 @@ struct AdapterParams {
     const float* scale;
     const int32_t* ranks;
     float* h;                    // M x n_parts x max_rank
+    int* status;                 // device status word
     long long ldx, ldbase, ldy;
     int M, K, N, n_slots, max_rank, n_parts;
     int part_end[kMaxBatch];     // column behind each part
