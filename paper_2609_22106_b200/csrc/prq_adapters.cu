@@ -1,6 +1,18 @@
-// Low-rank adapters beside a projection: h = x A^T of each row's adapter, then y = base + scale * h B^T.
+// Low-rank adapters beside a projection: h = scale * x A^T with the adapter of each row, then y = base + h B^T.
+//
+// Two launches.  The first one finds, for each of its clusters, an item -- rows of one adapter, from anywhere in a window of 4096 rows -- and sums
+// h of its rows; the second one streams y past h.  Items are worked out on the device, so that a captured call follows its row table.
+// Sums are fp32; h goes into the second product as two bf16 terms (hi = bf16(h), lo = bf16(h - hi): 16 bits and more of its
+// significand), whose products with B the tensor cores sum in fp32.
+//
+// Both products use mma.sync (16 x 8 x 16, bf16): with a rank of 16 to 64 they hold 16 to 128 flop per byte of y, too little for
+// its rate to become the bound.  Rows may stand in any order, and sums stay in the registers of the lane that stores them.  The order
+// of a reduction's elements is free, so the k index of every fragment is permuted such that a lane's share of a row is 16 (or 8)
+// contiguous bytes in both operands.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+
+#include <type_traits>
 
 #include "prq_internal.h"
 #include "prq_kernels.h"
@@ -9,86 +21,746 @@
 namespace prq {
 namespace {
 
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 __device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
-__device__ __forceinline__ int rank_of(const AdapterParams& p, int slot) {
-    return p.ranks ? min(max(p.ranks[slot], 0), p.max_rank) : p.max_rank;
-}
-
-// h[m, p, r] = scale * sum_k x[m, k] A[p, r, k]: a block per row, a warp per (p, r).
-__global__ void __launch_bounds__(256) adapters_h_kernel(const __grid_constant__ AdapterParams p) {
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const long long m = blockIdx.x;
-    const int slot = p.row_adapter[m];
-    if (slot < 0 || slot >= p.n_slots) return;
-    const int rank = rank_of(p, slot), lane = threadIdx.x & 31;
-    const float scale = p.scale ? p.scale[slot] : 1.0f;
-    for (int i = threadIdx.x >> 5; i < p.n_parts * rank; i += 8) {
-        const int part = i / rank, r = i - part * rank;
-        const uint4* a = reinterpret_cast<const uint4*>(p.A + ((static_cast<long long>(slot) * p.n_parts + part) * p.max_rank + r) * p.K);
-        const uint4* x = reinterpret_cast<const uint4*>(p.x + m * p.ldx);
-        float sum = 0.0f;
-        for (int k = lane; k < p.K / 8; k += 32) {
-            const uint4 va = a[k], vx = x[k];
-            const uint32_t *wa = &va.x, *wx = &vx.x;
+// Eight columns of y as they are stored.
+template <class T>
+struct Columns {
+    uint4 raw[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                sum = fmaf(bf16_lo(wa[j]), bf16_lo(wx[j]), sum);
-                sum = fmaf(bf16_hi(wa[j]), bf16_hi(wx[j]), sum);
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) raw[i] = reinterpret_cast<const uint4*>(p)[i];
+    }
+    __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) reinterpret_cast<uint4*>(p)[i] = raw[i];
+    }
+    // the sum is rounded once, to nearest
+    __device__ __forceinline__ void add(const float (&d)[8]) {
+        if constexpr (sizeof(T) == 2) {
+            uint32_t* w = &raw[0].x;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = pack_bf16(bf16_lo(w[i]) + d[2 * i], bf16_hi(w[i]) + d[2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t* w = &raw[i / 4].x + i % 4;
+                *w = __float_as_uint(__uint_as_float(*w) + d[i]);
             }
         }
+    }
+};
+
+// ---------------------------------------------------------------- items
+// Up to 16 rows each where a call has few of them, so that there are many items; up to 128 otherwise, so that A and B are read seldom.
+constexpr int kFewRows = 16, kManyRows = 128;
+constexpr int kFewCall = 128;         // rows of a call up to which items are small
+constexpr int kWindow = 4096;         // rows that are put in the order of their adapters together
+constexpr int kSortedSlots = 511;     // pools of more adapters, and calls of up to 32 rows: 32 rows that follow one another are grouped
+
+struct __align__(16) Item {
+    int slot, rows, rank, pad;        // rows: 0 -- no such item; rank: 0 -- no adapter
+    int row[kManyRows];
+};
+
+// rows per window, items that a window may have, windows, items in all (-1: too many)
+AdapterItems plan_items(int M, int n_slots) {
+    AdapterItems t;
+    if (n_slots > kSortedSlots) {
+        t.window = M < 32 ? M : 32;
+        t.per_window = t.window;
+    } else {
+        t.window = M < kWindow ? M : kWindow;
+        const int kinds = n_slots + 1 < t.window ? n_slots + 1 : t.window;
+        t.per_window = t.window / (M <= kFewCall ? kFewRows : kManyRows) + kinds;   // whole ones, and a rest of each adapter
+    }
+    t.windows = static_cast<int>((M + static_cast<long long>(t.window) - 1) / t.window);
+    const long long n = static_cast<long long>(t.windows) * t.per_window;
+    t.n = n > 0x7fffffffll / 16 ? -1 : static_cast<int>(n);
+    return t;
+}
+
+constexpr int kHThreads = 512, kHWarps = kHThreads / 32, kSteps = kWindow / kHThreads;
+
+struct FindShared {
+    uint16_t count[kHWarps][kSortedSlots + 1];   // rows per warp and adapter (the last one: none), then the rows in front of them
+    int warp_items[kHWarps];
+    int slot, first, rows;
+    int row[kManyRows];
+};
+
+// The CTA's item: the index-th one of the window at m0.  Every thread keeps up to kSteps rows and their places among the rows of
+// their adapter (a warp's rows follow one another, so that the order is that of the rows and a prompt's stay together).
+template <int kItemRows>
+__device__ __forceinline__ void find_item(const AdapterParams& p, int m0, int n, int index, FindShared& f) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kinds = p.n_slots + 1;
+    const int steps = (n + kHThreads - 1) / kHThreads, begin = warp * steps * 32;
+    int slot[kSteps], place[kSteps];
+    unsigned same[kSteps];
 #pragma unroll
-        for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (lane == 0) p.h[(m * p.n_parts + part) * p.max_rank + r] = sum * scale;
+    for (int s = 0; s < kSteps; ++s) {
+        const int m = begin + 32 * s + lane;
+        slot[s] = -1;
+        if (s < steps && m < n) slot[s] = p.row_adapter[m0 + m];
+    }
+    for (int i = lane; i < kinds; i += 32) f.count[warp][i] = 0;
+    if (threadIdx.x == 0) f.rows = 0;
+    __syncwarp();
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        if (s >= steps) break;
+        const bool inside = begin + 32 * s + lane < n;
+        if (inside && static_cast<unsigned>(slot[s]) >= static_cast<unsigned>(p.n_slots)) slot[s] = p.n_slots;
+        if (!inside) slot[s] = -1;
+        same[s] = __match_any_sync(0xffffffffu, slot[s]);
+    }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        if (s >= steps) break;
+        const int leader = __ffs(same[s]) - 1;
+        int at = 0;
+        if (lane == leader && slot[s] >= 0) {
+            at = f.count[warp][slot[s]];
+            f.count[warp][slot[s]] = static_cast<uint16_t>(at + __popc(same[s]));
+        }
+        place[s] = __shfl_sync(0xffffffffu, at, leader) + __popc(same[s] & ((1u << lane) - 1));
+        __syncwarp();
+    }
+    __syncthreads();
+    // a thread per adapter: its rows in front of each warp, its items, and the items of the adapters before it
+    int rows = 0;
+    const int kind = threadIdx.x;
+    if (kind < kinds) {
+#pragma unroll
+        for (int w = 0; w < kHWarps; ++w) {
+            const int c = f.count[w][kind];
+            f.count[w][kind] = static_cast<uint16_t>(rows);
+            rows += c;
+        }
+    }
+    const int items = (rows + kItemRows - 1) / kItemRows;
+    int sum = items;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, d);
+        if (lane >= d) sum += v;
+    }
+    if (lane == 31) f.warp_items[warp] = sum;
+    __syncthreads();
+    int first = sum - items;
+#pragma unroll
+    for (int w = 0; w < kHWarps; ++w) first += w < warp ? f.warp_items[w] : 0;
+    if (index >= first && index < first + items) {
+        f.slot = kind;
+        f.first = (index - first) * kItemRows;
+        f.rows = min(kItemRows, rows - f.first);
+    }
+    __syncthreads();
+    if (f.rows > 0) {
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+            if (s >= steps) break;
+            if (slot[s] != f.slot) continue;
+            const int at = f.count[warp][slot[s]] + place[s] - f.first;
+            if (at >= 0 && at < kItemRows) f.row[at] = m0 + begin + 32 * s + lane;
+        }
+    }
+    __syncthreads();
+}
+
+// The same within 32 rows that follow one another, for any number of adapters, by one warp: items in the order of their first rows.
+template <int kItemRows>
+__device__ __forceinline__ void find_item_of_32(const AdapterParams& p, int m0, int n, int index, FindShared& f) {
+    if (threadIdx.x < 32) {
+        const int lane = threadIdx.x;
+        int slot = lane < n ? p.row_adapter[m0 + lane] : -2;
+        if (lane < n && static_cast<unsigned>(slot) >= static_cast<unsigned>(p.n_slots)) slot = -1;
+        const unsigned same = __match_any_sync(0xffffffffu, slot), before = (1u << lane) - 1;
+        const int nth = __popc(same & before);
+        const bool leads = lane < n && nth % kItemRows == 0;
+        const unsigned leaders = __ballot_sync(0xffffffffu, leads);
+        const bool chosen = leads && __popc(leaders & before) == index;
+        const unsigned who = __ballot_sync(0xffffffffu, chosen);
+        if (lane == 0) f.rows = 0;
+        __syncwarp();
+        if (who) {
+            const int first = __shfl_sync(0xffffffffu, nth, __ffs(who) - 1);
+            if ((same & who) && nth >= first && nth < first + kItemRows) f.row[nth - first] = m0 + lane;
+            if (chosen) {
+                f.slot = slot;
+                f.rows = min(kItemRows, __popc(same) - nth);
+            }
+        }
+    }
+    __syncthreads();
+}
+
+struct Workspace {
+    Item* items;
+    uint4* h;          // M x ranks / 4: (hi, lo) of four ranks
+};
+__host__ __device__ inline Workspace views(void* at, int n_items) {
+    return Workspace{static_cast<Item*>(at), reinterpret_cast<uint4*>(static_cast<uint8_t*>(at) + sizeof(Item) * n_items)};
+}
+
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int n>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory"); }
+
+// ---------------------------------------------------------------- h
+// An item and 8 kRankTiles ranks per cluster, whose CTAs split K.  Rows of x and of A come into a ring in shared memory, kStageK of K at a
+// time; what is on its way at once is what sets the pace, so that few rows come in long pieces.  A warp has 16 rows and one 32 of K in
+// kWarpsK.  Row stride in the ring: 64 bytes off a multiple of 128, so that the eight lanes of a 16-byte load (two rows, four lanes
+// each) meet no bank twice.
+template <int kRankTiles, int kItemRows>
+struct HShared {
+    static constexpr int kRanks = 8 * kRankTiles, kRows = kItemRows + kRanks;
+    static constexpr int kStageK = kItemRows == kFewRows ? 512 : 128, kStages = kItemRows == kFewRows ? 2 : 3;
+    static constexpr int kRowBytes = 2 * kStageK + 64, kTiles = kItemRows / 16, kWarpsK = kHWarps / kTiles;
+    union {
+        uint8_t ring[kStages][kRows][kRowBytes];
+        FindShared find;
+        float part[kWarpsK][kItemRows][kRanks + 4];   // sums of the warps
+    };
+    float4 got[kItemRows * kRanks / 4 + 8];   // sums of the cluster's CTAs for this CTA's share of them, one CTA behind the other
+    int row[kItemRows];
+};
+template <int kRankTiles, int kItemRows>
+__global__ void __launch_bounds__(kHThreads, 1) adapters_h_kernel(const __grid_constant__ AdapterParams p) {
+    using Shared = HShared<kRankTiles, kItemRows>;
+    constexpr int kRanks = Shared::kRanks, kRows = Shared::kRows, kStageK = Shared::kStageK, kStages = Shared::kStages, kRowBytes = Shared::kRowBytes;
+    constexpr int kTiles = Shared::kTiles, kWarpsK = Shared::kWarpsK;
+    extern __shared__ __align__(128) uint8_t smem[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int ctas = p.cluster, cta = cluster_ctarank(), index = blockIdx.x / ctas, r0 = blockIdx.y * kRanks;
+    const int pad_rank = p.pad_rank, ranks = p.n_parts * pad_rank;
+    const Workspace ws = views(p.h, p.items.n);
+    const int window = p.items.windows == 1 ? 0 : index / p.items.per_window, m0 = window * p.items.window, n = min(p.items.window, p.M - m0);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
+    const int nth = index - window * p.items.per_window;
+    if (p.n_slots > kSortedSlots || p.M <= 32) find_item_of_32<kItemRows>(p, m0, n, nth, sh.find);
+    else find_item<kItemRows>(p, m0, n, nth, sh.find);
+    const int slot = sh.find.slot, rows = sh.find.rows;
+    const int rank = rows == 0 || slot < 0 || slot >= p.n_slots ? 0 : p.ranks ? min(max(p.ranks[slot], 0), p.max_rank) : p.max_rank;
+    // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
+    const int steps = rank > 0 ? p.K / 32 : 0, k0 = steps * cta / ctas * 32, k1 = steps * (cta + 1) / ctas * 32;
+    const int stages = (k1 - k0 + kStageK - 1) / kStageK;
+    auto part_of = [&](int f) { return (f >= pad_rank) + (f >= 2 * pad_rank) + (f >= 3 * pad_rank); };
+    // a thread has the same 16 bytes of every kAtOnce-th row in each stage
+    constexpr int kPieces = kStageK / 8, kAtOnce = kHThreads / kPieces, kMine = (kRows + kAtOnce - 1) / kAtOnce;
+    const int piece = threadIdx.x % kPieces, my_row = threadIdx.x / kPieces;
+    const uint16_t* from[kMine];   // null: no such row
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int r = my_row + i * kAtOnce, f = r0 + r - kItemRows, part = part_of(f), k = f - part * pad_rank;
+        from[i] = nullptr;
+        if (r < kItemRows) {
+            if (r < rows) from[i] = p.x + sh.find.row[r] * p.ldx + k0 + 8 * piece;
+        } else if (r < kRows && f < ranks && k < rank) {
+            from[i] = p.A + ((static_cast<long long>(slot) * p.n_parts + part) * p.max_rank + k) * p.K + k0 + 8 * piece;
+        }
+    }
+    if (static_cast<int>(threadIdx.x) < rows) {
+        const int m = sh.find.row[threadIdx.x];
+        sh.row[threadIdx.x] = m;
+        if (cta == 0 && blockIdx.y == 0) ws.items[index].row[threadIdx.x] = m;
+    }
+    if (cta == 0 && blockIdx.y == 0 && threadIdx.x == 0) *reinterpret_cast<int4*>(&ws.items[index]) = make_int4(slot, rows, rank, 0);
+    __syncthreads();   // (the ring takes the table's memory)
+    const uint32_t to = smem_u32(sh.ring[0][0]) + my_row * kRowBytes + 16 * piece;
+    auto ask = [&](int stage, int place) {
+        if (stage < stages && k0 + stage * kStageK + 8 * piece < k1) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                if (from[i]) copy16(to + place * (kRows * kRowBytes) + i * kAtOnce * kRowBytes, from[i] + stage * kStageK);
+            }
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kStages - 1; ++i) ask(i, i);
+
+    float acc[kRankTiles][4];
+#pragma unroll
+    for (int t = 0; t < kRankTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[t][i] = 0.0f;
+    const int tile = warp % kTiles, kw = warp / kTiles;
+    int place = 0;
+    for (int s = 0; s < stages; ++s) {
+        copies_wait<kStages - 2>();
+        __syncthreads();   // this stage is there for all, and the one before it has been read
+        ask(s + kStages - 1, place == 0 ? kStages - 1 : place - 1);
+        const int here = min(kStageK, k1 - k0 - s * kStageK);
+        if (tile * 16 < rows) {
+            const uint8_t* at = sh.ring[place][0] + 16 * q;
+#pragma unroll
+            for (int c = 0; c < kStageK / 32 / kWarpsK; ++c) {
+                const int k = 32 * (c * kWarpsK + kw);   // (what ranks and rows that do not exist leave there reaches no sum that is read)
+                if (k >= here) break;
+                const uint4 va = *reinterpret_cast<const uint4*>(at + (16 * tile + g) * kRowBytes + 2 * k);
+                const uint4 vb = *reinterpret_cast<const uint4*>(at + (16 * tile + 8 + g) * kRowBytes + 2 * k);
+#pragma unroll
+                for (int t = 0; t < kRankTiles; ++t) {
+                    const uint4 a = *reinterpret_cast<const uint4*>(at + (kItemRows + 8 * t + g) * kRowBytes + 2 * k);
+                    mma_bf16(acc[t], va.x, vb.x, va.y, vb.y, a.x, a.y);
+                    mma_bf16(acc[t], va.z, vb.z, va.w, vb.w, a.z, a.w);
+                }
+            }
+        }
+        place = place == kStages - 1 ? 0 : place + 1;
+    }
+    copies_wait<0>();
+    __syncthreads();
+    // sums of the CTA, then those of the cluster, a share of them in each CTA; scaled, and split in two terms
+    if (tile * 16 < rows) {
+#pragma unroll
+        for (int t = 0; t < kRankTiles; ++t)
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+                *reinterpret_cast<float2*>(&sh.part[kw][16 * tile + 8 * k + g][8 * t + 2 * q]) = make_float2(acc[t][2 * k], acc[t][2 * k + 1]);
+    }
+    __syncthreads();
+    const int quads = (rank > 0 ? rows : 0) * (kRanks / 4), share = (quads + ctas - 1) / ctas;   // sums of four ranks of a row; a CTA's share of them
+    const float to_share = share > 0 ? 1.0f / share : 0.0f;
+    if (ctas > 1) cluster_wait();
+    for (int i = threadIdx.x; i < quads; i += kHThreads) {
+        const int m = i / (kRanks / 4), j = i % (kRanks / 4) * 4;
+        float4 sum = *reinterpret_cast<const float4*>(&sh.part[0][m][j]);
+#pragma unroll
+        for (int k = 1; k < kWarpsK; ++k) {
+            const float4 u = *reinterpret_cast<const float4*>(&sh.part[k][m][j]);
+            sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+        }
+        const int c = __float2int_rd((i + 0.5f) * to_share);   // i / share (i + 0.5 is 2^-13 of itself and more away from a border)
+        st_cluster(cluster_map(smem_u32(&sh.got[cta * share + i - c * share]), c), sum);
+    }
+    const float scale = rank > 0 && p.scale ? p.scale[slot] : 1.0f;
+    if (ctas > 1) {
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
+    const int i0 = min(quads, share * cta), mine = min(quads, i0 + share) - i0;
+    for (int i = threadIdx.x; i < mine; i += kHThreads) {
+        const int m = (i0 + i) / (kRanks / 4), f = r0 + (i0 + i) % (kRanks / 4) * 4, r = f - part_of(f) * pad_rank;
+        if (f >= ranks) continue;
+        float4 sum = sh.got[i];
+        for (int k = 1; k < ctas; ++k) {
+            const float4 u = sh.got[k * share + i];
+            sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+        }
+        const float v[4] = {r < rank ? sum.x * scale : 0.0f, r + 1 < rank ? sum.y * scale : 0.0f, r + 2 < rank ? sum.z * scale : 0.0f, r + 3 < rank ? sum.w * scale : 0.0f};
+        uint4 h;
+        h.x = pack_bf16(v[0], v[1]);
+        h.y = pack_bf16(v[2], v[3]);
+        h.z = pack_bf16(v[0] - bf16_lo(h.x), v[1] - bf16_hi(h.x));
+        h.w = pack_bf16(v[2] - bf16_lo(h.y), v[3] - bf16_hi(h.y));
+        ws.h[static_cast<long long>(sh.row[m]) * (ranks / 4) + f / 4] = h;
     }
 }
 
+// ---------------------------------------------------------------- y
+// In both kernels a lane has eight columns that follow one another: column 2 q + e of the j-th 8-column fragment stands for column 8 q + 2 j + e
+// of a block of 32.  bf16: the accumulators begin with base (their sum is cut to 24 bits, and then rounded to 8); fp32: base is added to
+// the sum.  What lies behind an adapter's rank may be anything: `masked` clears it in a lane's four ranks of B.
+__device__ __forceinline__ uint2 masked(uint2 b, int left) {
+    b.x &= left >= 2 ? 0xffffffffu : left == 1 ? 0xffffu : 0u;
+    b.y &= left >= 4 ? 0xffffffffu : left == 3 ? 0xffffu : 0u;
+    return b;
+}
 template <class T>
-__global__ void __launch_bounds__(256) adapters_y_kernel(const __grid_constant__ AdapterParams p) {
+__device__ __forceinline__ void begin_sum(float (&acc)[4][4], const Columns<T>& v, int e) {   // e: 0 -- row g, 2 -- row g + 8
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t w[4] = {v.raw[0].x, v.raw[0].y, v.raw[0].z, v.raw[0].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            acc[j][e] = bf16_lo(w[j]);
+            acc[j][e + 1] = bf16_hi(w[j]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j][e] = acc[j][e + 1] = 0.0f;
+    }
+}
+template <class T>
+__device__ __forceinline__ Columns<T> end_sum(const float (&acc)[4][4], const Columns<T>& v, int e) {
+    Columns<T> to;
+    if constexpr (sizeof(T) == 2) {
+        to.raw[0] = make_uint4(pack_bf16(acc[0][e], acc[0][e + 1]), pack_bf16(acc[1][e], acc[1][e + 1]), pack_bf16(acc[2][e], acc[2][e + 1]),
+                               pack_bf16(acc[3][e], acc[3][e + 1]));
+    } else {
+        const float d[8] = {acc[0][e], acc[0][e + 1], acc[1][e], acc[1][e + 1], acc[2][e], acc[2][e + 1], acc[3][e], acc[3][e + 1]};
+        to = v;
+        to.add(d);
+    }
+    return to;
+}
+// The last columns of a matrix whose width is no multiple of eight (their accumulators began with zero).
+template <class T>
+__device__ __forceinline__ void add_last(const float (&acc)[4][4], int e, int cols, const T* from, T* to) {
+#pragma unroll
+    for (int n = 0; n < 8; ++n)
+        if (n < cols) to[n] = static_cast<T>(static_cast<float>(from[n]) + acc[n / 2][e + (n & 1)]);
+}
+// Part and columns of the unit-th `width` columns of y.
+struct Unit { int part, n0, end; };
+__device__ __forceinline__ Unit unit_of(const AdapterParams& p, int unit, int width) {
+    int part = 0, from = 0;
+#pragma unroll
+    for (int i = 0; i < kMaxBatch - 1; ++i) {
+        if (part != i || i >= p.n_parts - 1) continue;
+        const int n = (p.part_end[i] - from + width - 1) / width;
+        if (unit >= n) {
+            unit -= n;
+            from = p.part_end[i];
+            ++part;
+        }
+    }
+    return Unit{part, from + width * unit, p.part_end[part]};
+}
+// Rows without an adapter, where y is not base: copied bit for bit.
+template <class T>
+__device__ __forceinline__ void copy_rows(const AdapterParams& p, const int* row, int rows, int n0, int n1, int thread, int threads) {
+    constexpr int kPiece = 16 / sizeof(T);
+    const int pieces = (n1 - n0 + kPiece - 1) / kPiece;
+    for (int i = thread; i < rows * pieces; i += threads) {
+        const int m = i / pieces, n = n0 + (i - m * pieces) * kPiece;
+        const T* from = static_cast<const T*>(p.base) + row[m] * p.ldbase + n;
+        T* to = static_cast<T*>(p.y) + row[m] * p.ldy + n;
+        if (n + kPiece <= n1) {
+            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+        } else {
+            for (int j = 0; n + j < n1; ++j) to[j] = from[j];
+        }
+    }
+}
+
+// Few rows: an item of up to 16 rows and 64 columns per warp, everything straight from memory.
+constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32;
+template <class T>
+__global__ void __launch_bounds__(kFewThreads, 4) adapters_few_y_kernel(const __grid_constant__ AdapterParams p, int units) {
+    const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int pad_rank = p.pad_rank, quads = p.n_parts * pad_rank / 4;
+    const Workspace ws = views(p.h, p.items.n);
+    const int ctas = (units + kFewWarps - 1) / kFewWarps, index = blockIdx.x / ctas, unit = (blockIdx.x - index * ctas) * kFewWarps + (threadIdx.x >> 5);
+    const Unit at = unit_of(p, unit, 64);
+    const Item& item = ws.items[index];
     grid_dependency_wait();
     grid_launch_dependents();
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= p.N) return;
-    int part = 0;
-    while (n >= p.part_end[part]) ++part;
-    for (long long m = blockIdx.y; m < p.M; m += gridDim.y) {
-        const int slot = p.row_adapter[m];
-        const int rank = slot < 0 || slot >= p.n_slots ? 0 : rank_of(p, slot);
-        const T* from = static_cast<const T*>(p.base) + m * p.ldbase + n;
-        T* to = static_cast<T*>(p.y) + m * p.ldy + n;
-        if (rank == 0) {
-            if (to != from) *to = *from;
-            continue;
-        }
-        const float* h = p.h + (m * p.n_parts + part) * p.max_rank;
-        const uint16_t* b = p.B + (static_cast<long long>(slot) * p.N + n) * p.max_rank;
-        float sum = 0.0f;
-        for (int r = 0; r < rank; ++r) sum = fmaf(h[r], __uint_as_float(static_cast<uint32_t>(b[r]) << 16), sum);
-        *to = static_cast<T>(static_cast<float>(*from) + sum);
+    const int4 head = *reinterpret_cast<const int4*>(&item);
+    int row[2] = {item.row[g], item.row[8 + g]};
+    const int other = item.row[0];
+    const int slot = head.x, rows = head.y, rank = head.z;
+    if (unit >= units || rows == 0) return;
+    if (rank == 0) {
+        if (p.base != p.y) copy_rows<T>(p, item.row, rows, at.n0, min(at.end, at.n0 + 64), lane, 32);
+        return;
     }
+    // (lanes whose row does not exist repeat the item's first one up to the store)
+    const bool mine[2] = {g < rows, 8 + g < rows};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) row[i] = mine[i] ? row[i] : other;
+    Columns<T> v[2][2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int col = at.n0 + 32 * j + 8 * q;
+            v[i][j] = Columns<T>{};
+            if (mine[i] && col + 8 <= at.end) v[i][j].load(static_cast<const T*>(p.base) + row[i] * p.ldbase + col);
+        }
+    float acc[2][4][4];
+    const uint16_t* B = p.B + (static_cast<long long>(slot) * p.N + at.n0 + 8 * (g >> 1) + (g & 1)) * p.max_rank + 4 * q;
+    const uint4* H = ws.h + at.part * (pad_rank / 4) + q;
+    const int n_left = at.end - at.n0 - 8 * (g >> 1) - (g & 1);   // columns of this lane's row of B up to the end
+#pragma unroll 1
+    for (int k = 0; k < rank; k += 16) {
+        const int left = rank - k - 4 * q;
+        uint2 b[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int n = 32 * (j / 4) + 2 * (j % 4);
+            b[j] = make_uint2(0, 0);
+            if (n < n_left && left > 0) b[j] = *reinterpret_cast<const uint2*>(B + static_cast<long long>(n) * p.max_rank + k);
+        }
+        const uint4 ha = H[static_cast<long long>(row[0]) * quads + k / 4], hb = H[static_cast<long long>(row[1]) * quads + k / 4];
+        if (k == 0) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) begin_sum<T>(acc[j], v[i][j], 2 * i);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (left < 4) b[j] = masked(b[j], left);
+            mma_bf16(acc[j / 4][j % 4], ha.x, hb.x, ha.y, hb.y, b[j].x, b[j].y);
+            mma_bf16(acc[j / 4][j % 4], ha.z, hb.z, ha.w, hb.w, b[j].x, b[j].y);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int col = at.n0 + 32 * j + 8 * q, cols = at.end - col;
+            if (!mine[i] || cols <= 0) continue;
+            T* to = static_cast<T*>(p.y) + row[i] * p.ldy + col;
+            if (cols >= 8) end_sum<T>(acc[j], v[i][j], 2 * i).store(to);
+            else add_last<T>(acc[j], 2 * i, cols, static_cast<const T*>(p.base) + row[i] * p.ldbase + col, to);
+        }
+}
+
+// Many rows: a CTA has an item and `span` tiles of kCols columns of one part.  Tiles of base and B come into a ring in shared memory; a
+// warp has 16 of the item's rows, whose h it keeps in registers, and all columns.  In the ring a row of B stands where the fragment's
+// lane wants it (row n of a block of 32 at 8 ((n % 8) / 2) + 2 (n / 8) + n % 2), with a stride of 32 bytes off a multiple of 64; of base,
+// odd rows have the halves of their 128 bytes swapped: no lane of a load meets another one's bank.
+constexpr int kManyThreads = 256, kManyStages = 3;
+template <class T>
+constexpr int kManyCols = 128 / sizeof(T);                           // 128 bytes of y per row and tile
+__host__ __device__ inline int b_stride(int max_rank) { return 2 * ((max_rank + 15) & ~15) + (max_rank % 32 <= 16 && max_rank % 32 > 0 ? 0 : 32); }
+template <class T>
+__host__ __device__ inline int many_stage_bytes(int max_rank) { return kManyRows * 128 + kManyCols<T> * b_stride(max_rank); }
+
+template <class T, int kSteps16>
+__global__ void __launch_bounds__(kManyThreads, kSteps16 == 1 ? 3 : 2) adapters_many_y_kernel(const __grid_constant__ AdapterParams p, int units, int span) {
+    constexpr int kCols = kManyCols<T>, kBlocks = kCols / 32, kPieceCols = 16 / sizeof(T);
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ const T* base_s[kManyRows];
+    __shared__ int row_s[kManyRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int pad_rank = p.pad_rank, quads = p.n_parts * pad_rank / 4, stride = b_stride(p.max_rank), stage_bytes = many_stage_bytes<T>(p.max_rank);
+    const Workspace ws = views(p.h, p.items.n);
+    const int index = blockIdx.x / units;
+    const Unit at = unit_of(p, blockIdx.x - index * units, kCols * span);
+    const Item& item = ws.items[index];
+    const int stop = min(at.end, at.n0 + kCols * span), tiles = (stop - at.n0 + kCols - 1) / kCols;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int4 head = *reinterpret_cast<const int4*>(&item);
+    const int listed = threadIdx.x < kManyRows ? item.row[threadIdx.x] : 0;
+    const int slot = head.x, rows = head.y, rank = head.z;
+    if (rows == 0) return;
+    if (rank == 0) {
+        if (p.base != p.y) copy_rows<T>(p, item.row, rows, at.n0, stop, threadIdx.x, kManyThreads);
+        return;
+    }
+    if (static_cast<int>(threadIdx.x) < rows) {
+        row_s[threadIdx.x] = listed;
+        base_s[threadIdx.x] = static_cast<const T*>(p.base) + listed * p.ldbase + at.n0;
+    }
+    __syncthreads();
+
+    // a thread copies one piece of every kRowStep-th row of base, and of one row of B one in kBThreads
+    constexpr int kRowStep = kManyThreads / 8, kBThreads = kManyThreads / kCols;
+    const int piece = threadIdx.x & 7, b_row = threadIdx.x / kBThreads, in = b_row & 31;
+    const T* base_from[kManyRows / kRowStep];
+#pragma unroll
+    for (int i = 0; i < kManyRows / kRowStep; ++i) {
+        const int r = (threadIdx.x >> 3) + i * kRowStep;
+        base_from[i] = r < rows ? base_s[r] + piece * kPieceCols : nullptr;
+    }
+    const uint32_t base_to = smem_u32(smem) + (threadIdx.x >> 3) * 128 + 16 * (piece ^ ((threadIdx.x >> 3 & 1) << 2));   // (kRowStep is even)
+    const uint16_t* b_from = p.B + (static_cast<long long>(slot) * p.N + at.n0 + b_row) * p.max_rank + 8 * (threadIdx.x % kBThreads);
+    const uint32_t b_to = smem_u32(smem) + kManyRows * 128 + ((b_row & ~31) + 8 * ((in & 7) >> 1) + 2 * (in >> 3) + (in & 1)) * stride + 16 * (threadIdx.x % kBThreads);
+    const int b_pieces = p.max_rank / 8 - threadIdx.x % kBThreads, width = stop - at.n0;
+    auto ask = [&](int tile, int place) {
+        const int n = tile * kCols;
+        if (n + (piece + 1) * kPieceCols <= width) {
+#pragma unroll
+            for (int i = 0; i < kManyRows / kRowStep; ++i)
+                if (base_from[i]) copy16(base_to + place * stage_bytes + i * (kRowStep * 128), base_from[i] + n);
+        }
+        if (n + b_row < width) {
+            const uint16_t* b = b_from + static_cast<long long>(n) * p.max_rank;
+            for (int i = 0; i < b_pieces; i += kBThreads) copy16(b_to + place * stage_bytes + 16 * i, b + 8 * i);
+        }
+        copies_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < kManyStages - 1; ++i) ask(i, i);
+
+    // h of rows g and 8 + g of the warp's 16 (of a row that exists, where they do not)
+    const int ra = 16 * warp + g, rb = ra + 8;
+    const bool working = 16 * warp < rows, has_a = ra < rows, has_b = rb < rows;
+    const long long ma = working ? row_s[has_a ? ra : 0] : 0, mb = working ? row_s[has_b ? rb : 0] : 0;
+    uint4 ha[kSteps16], hb[kSteps16];
+    if (working) {
+        const uint4* H = ws.h + at.part * (pad_rank / 4) + q;
+#pragma unroll
+        for (int k = 0; k < kSteps16; ++k) {
+            ha[k] = hb[k] = make_uint4(0, 0, 0, 0);
+            if (16 * k < rank) {
+                ha[k] = H[ma * quads + 4 * k];
+                hb[k] = H[mb * quads + 4 * k];
+            }
+        }
+    }
+    T* ya = static_cast<T*>(p.y) + ma * p.ldy + at.n0 + 8 * q;
+    T* yb = static_cast<T*>(p.y) + mb * p.ldy + at.n0 + 8 * q;
+    const uint32_t swap = (ra & 1) << 6;   // (rb's is the same)
+    int place = 0;
+    // one tile; `whole`: all of its columns, and all of the rank's steps, exist
+    auto one_tile = [&](int tile, auto whole) {
+        constexpr bool kWhole = decltype(whole)::value;
+        const uint8_t *a_s = smem + place * stage_bytes + ra * 128, *b_s = smem + place * stage_bytes + kManyRows * 128 + g * stride + 8 * q;
+        const int n = tile * kCols;
+#pragma unroll
+        for (int block = 0; block < kBlocks; ++block) {
+            const int cols = kWhole ? 8 : width - n - 32 * block - 8 * q;   // from this lane's first one up to the end
+            Columns<T> va, vb;
+#pragma unroll
+            for (int i = 0; i < 8 / kPieceCols; ++i) {   // (8 columns: one piece of bf16, two of fp32)
+                const uint32_t off = (static_cast<uint32_t>((32 * block + 8 * q) / kPieceCols + i) * 16) ^ swap;
+                va.raw[i] = vb.raw[i] = make_uint4(0, 0, 0, 0);
+                if (cols >= 8) {
+                    va.raw[i] = *reinterpret_cast<const uint4*>(a_s + off);
+                    vb.raw[i] = *reinterpret_cast<const uint4*>(a_s + 8 * 128 + off);
+                }
+            }
+            float acc[4][4];
+            begin_sum<T>(acc, va, 0);
+            begin_sum<T>(acc, vb, 2);
+#pragma unroll
+            for (int k = 0; k < kSteps16; ++k) {
+                if (!kWhole && 16 * k >= rank) break;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint2 b = *reinterpret_cast<const uint2*>(b_s + (32 * block + 8 * j) * stride + 32 * k);
+                    if (!kWhole && rank - 16 * k < 16) b = masked(b, rank - 16 * k - 4 * q);
+                    mma_bf16(acc[j], ha[k].x, hb[k].x, ha[k].y, hb[k].y, b.x, b.y);
+                    mma_bf16(acc[j], ha[k].z, hb[k].z, ha[k].w, hb[k].w, b.x, b.y);
+                }
+            }
+            if (cols >= 8) {
+                if (has_a) end_sum<T>(acc, va, 0).store(ya + n + 32 * block);
+                if (has_b) end_sum<T>(acc, vb, 2).store(yb + n + 32 * block);
+            } else if (cols > 0) {
+                const T* from = static_cast<const T*>(p.base) + at.n0 + n + 32 * block + 8 * q;
+                if (has_a) add_last<T>(acc, 0, cols, from + ma * p.ldbase, ya + n + 32 * block);
+                if (has_b) add_last<T>(acc, 2, cols, from + mb * p.ldbase, yb + n + 32 * block);
+            }
+        }
+    };
+#pragma unroll 1
+    for (int tile = 0; tile < tiles; ++tile) {
+        copies_wait<kManyStages - 2>();
+        __syncthreads();   // this tile is there for all, and the one before it has been read
+        ask(tile + kManyStages - 1, place == 0 ? kManyStages - 1 : place - 1);
+        if (working) {
+            if (rank == 16 * kSteps16 && (tile + 1) * kCols <= width) one_tile(tile, std::true_type());
+            else one_tile(tile, std::false_type());
+        }
+        place = place == kManyStages - 1 ? 0 : place + 1;
+    }
+    copies_wait<0>();
+}
+
+template <class... Params, class... Args>
+cudaError_t launch_kernel(void (*kernel)(Params...), dim3 blocks, int threads, int cluster, size_t smem, cudaStream_t stream, const Args&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = blocks;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+template <int kRankTiles, int kItemRows>
+cudaError_t launch_h(const AdapterParams& p, int passes, cudaStream_t stream) {
+    static OncePerDevice once;
+    constexpr int kBytes = sizeof(HShared<kRankTiles, kItemRows>);
+    static_assert(kBytes <= 227 * 1024, "shared memory");
+    const auto kernel = adapters_h_kernel<kRankTiles, kItemRows>;
+    const cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes); });
+    if (e != cudaSuccess) return e;
+    return launch_kernel(kernel, dim3(p.items.n * p.cluster, passes), kHThreads, p.cluster, kBytes, stream, p);
+}
+template <int kItemRows>
+cudaError_t launch_h(const AdapterParams& p, cudaStream_t stream) {
+    const int ranks = p.n_parts * p.pad_rank, passes = (ranks + 63) / 64, tiles = (ranks / 8 + passes - 1) / passes;
+    return tiles <= 2 ? launch_h<2, kItemRows>(p, passes, stream) : tiles <= 4 ? launch_h<4, kItemRows>(p, passes, stream)
+         : tiles <= 6 ? launch_h<6, kItemRows>(p, passes, stream) : launch_h<8, kItemRows>(p, passes, stream);
+}
+template <class T, int kSteps16>
+cudaError_t launch_many_y(const AdapterParams& p, int units, int span, cudaStream_t stream) {
+    static OncePerDevice once;
+    const auto kernel = adapters_many_y_kernel<T, kSteps16>;
+    const cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kManyStages * many_stage_bytes<T>(PRQ_ADAPTER_MAX_RANK)); });
+    if (e != cudaSuccess) return e;
+    return launch_kernel(kernel, dim3(units * p.items.n), kManyThreads, 1, kManyStages * many_stage_bytes<T>(p.max_rank), stream, p, units, span);
+}
+template <class T>
+cudaError_t launch_y(const AdapterParams& p, int num_sms, cudaStream_t stream) {
+    const bool few = p.M <= kFewCall;
+    int span = 1;
+    if (!few) {
+        span = 4;
+        if (const char* v = dev_knobs_enabled() ? std::getenv("PRQ_AD_PER") : nullptr) span = atoi(v);
+    }
+    const int width = few ? 64 : kManyCols<T> * span;
+    int units = 0;
+    for (int i = 0; i < p.n_parts; ++i) units += (p.part_end[i] - (i ? p.part_end[i - 1] : 0) + width - 1) / width;
+    if (static_cast<long long>(units) * p.items.n > 0x7fffffffll) return cudaErrorInvalidValue;
+    if (few) return launch_kernel(adapters_few_y_kernel<T>, dim3((units + kFewWarps - 1) / kFewWarps * p.items.n), kFewThreads, 1, 0, stream, p, units);
+    const int steps = p.pad_rank / 16;
+    return steps == 1 ? launch_many_y<T, 1>(p, units, span, stream) : steps == 2 ? launch_many_y<T, 2>(p, units, span, stream)
+         : steps <= 4 ? launch_many_y<T, 4>(p, units, span, stream) : launch_many_y<T, 8>(p, units, span, stream);
 }
 
 }  // namespace
 
-size_t adapters_workspace_bytes(int M, int n_parts, int max_rank) { return sizeof(float) * M * n_parts * max_rank; }
+size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank) {
+    const AdapterItems items = plan_items(M, n_slots);
+    const size_t ranks = n_parts * ((max_rank + 15) & ~15);
+    return items.n < 0 ? 0 : sizeof(Item) * items.n + 4 * ranks * static_cast<size_t>(M);
+}
 
-cudaError_t launch_adapters(const AdapterParams& p, bool bf16, int num_sms, cudaStream_t stream, int* launches) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.stream = stream;
-    cfg.blockDim = dim3(256);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cfg.gridDim = dim3(p.M);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, adapters_h_kernel, p);
+cudaError_t launch_adapters(const AdapterParams& in, bool bf16, int num_sms, cudaStream_t stream, int* launches) {
+    AdapterParams p = in;
+    p.items = plan_items(p.M, p.n_slots);
+    p.pad_rank = (p.max_rank + 15) & ~15;
+    if (p.items.n < 1) return cudaErrorInvalidValue;
+    const bool few = p.M <= kFewCall;
+    const int passes = (p.n_parts * p.pad_rank + 63) / 64;
+    const int full = p.M / kManyRows, items = few ? p.items.n : full + std::min(p.n_slots, full) / 4 + 1;
+    p.cluster = 1;
+    for (int c = 2; c <= 8; ++c)
+        if (static_cast<long long>(items) * passes * c <= num_sms / 18 * (18 / c) * c && p.K / 32 >= (few ? 8 : 4) * c) p.cluster = c;
+    if (const char* v = dev_knobs_enabled() ? std::getenv("PRQ_AD_CLUSTER") : nullptr) p.cluster = atoi(v);
+    const cudaError_t e = few ? launch_h<kFewRows>(p, stream) : launch_h<kManyRows>(p, stream);
     if (e != cudaSuccess) return e;
-    cfg.gridDim = dim3((p.N + 255) / 256, std::min(p.M, 65535));
-    *launches = 2;
-    return bf16 ? cudaLaunchKernelEx(&cfg, adapters_y_kernel<__nv_bfloat16>, p) : cudaLaunchKernelEx(&cfg, adapters_y_kernel<float>, p);
+    ++*launches;
+    const cudaError_t e2 = bf16 ? launch_y<__nv_bfloat16>(p, num_sms, stream) : launch_y<float>(p, num_sms, stream);
+    if (e2 == cudaSuccess) ++*launches;
+    return e2;
 }
 
 }  // namespace prq

@@ -228,6 +228,7 @@ struct RotateParams {
 cudaError_t launch_rotate_heads(const RotateParams& p, bool interleaved, bool norm, bool bf16, int num_sms, cudaStream_t stream);
 
 // Low-rank adapters beside a projection (prq_adapters.cu).
+struct AdapterItems { int window, per_window, windows, n; };   // see prq_adapters.cu
 struct AdapterParams {
     const int32_t* row_adapter;
     const uint16_t* x;
@@ -237,13 +238,16 @@ struct AdapterParams {
     const uint16_t* B;           // n_slots x N x max_rank
     const float* scale;
     const int32_t* ranks;
-    float* h;                    // M x n_parts x max_rank
+    void* h;                     // the workspace
     int* status;                 // device status word
     long long ldx, ldbase, ldy;
     int M, K, N, n_slots, max_rank, n_parts;
+    int cluster;                 // CTAs per cluster
+    int pad_rank;                // max_rank in whole k steps of 16
+    AdapterItems items;
     int part_end[kMaxBatch];     // column behind each part
 };
-size_t adapters_workspace_bytes(int M, int n_parts, int max_rank);
+size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank);
 cudaError_t launch_adapters(const AdapterParams& p, bool bf16, int num_sms, cudaStream_t stream, int* launches);
 
 // Benchmark utility: `grid` CTAs each issuing n_mma block-scaled FP4 MMAs (128 x 256 x 64) from shared memory.
