@@ -224,68 +224,61 @@ template <int n>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(n) : "memory"); }
 
 // ---------------------------------------------------------------- h
-// An item and 8 kRankTiles ranks per cluster, whose CTAs split K.  Rows of x and of A come into a ring in shared memory, kStageK of K at a
-// time; what is on its way at once is what sets the pace, so that few rows come in long pieces.  A warp has 16 rows and one 32 of K in
-// kWarpsK.  Row stride in the ring: 64 bytes off a multiple of 128, so that the eight lanes of a 16-byte load (two rows, four lanes
-// each) meet no bank twice.
+// An item and 8 kRankTiles ranks at a time per cluster, whose CTAs split K.  Rows of x and of A come into a ring in shared memory, kStageK of K
+// at a time; a warp has 16 rows and one 32 of K in kWarpsK.  Few rows: what is on its way at once sets the pace (a CTA's share of K is a few
+// stages), so the pieces are long.  Row stride in the ring: 64 bytes off a multiple of 128, so that the eight lanes of a 16-byte load (two
+// rows, four lanes each) meet no bank twice.
 template <int kRankTiles, int kItemRows>
 struct HShared {
     static constexpr int kRanks = 8 * kRankTiles, kRows = kItemRows + kRanks;
-    static constexpr int kStageK = kItemRows == kFewRows ? 512 : 128, kStages = kItemRows == kFewRows ? 2 : 3;
+    static constexpr int kStageK = kItemRows == kFewRows ? 256 : 128, kStages = kItemRows == kFewRows && kRankTiles <= 6 ? 4 : 3;
     static constexpr int kRowBytes = 2 * kStageK + 64, kTiles = kItemRows / 16, kWarpsK = kHWarps / kTiles;
     union {
         uint8_t ring[kStages][kRows][kRowBytes];
         FindShared find;
         float part[kWarpsK][kItemRows][kRanks + 4];   // sums of the warps
     };
-    float4 got[kItemRows * kRanks / 4 + 8];   // sums of the cluster's CTAs for this CTA's share of them, one CTA behind the other
     int row[kItemRows];
 };
+struct Found { int slot, rows, rank; };
+// The cluster's item, its rows in sh.row.
 template <int kRankTiles, int kItemRows>
-__global__ void __launch_bounds__(kHThreads, 1) adapters_h_kernel(const __grid_constant__ AdapterParams p) {
-    using Shared = HShared<kRankTiles, kItemRows>;
-    constexpr int kRanks = Shared::kRanks, kRows = Shared::kRows, kStageK = Shared::kStageK, kStages = Shared::kStages, kRowBytes = Shared::kRowBytes;
-    constexpr int kTiles = Shared::kTiles, kWarpsK = Shared::kWarpsK;
-    extern __shared__ __align__(128) uint8_t smem[];
-    Shared& sh = *reinterpret_cast<Shared*>(smem);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-    const int ctas = p.cluster, cta = cluster_ctarank(), index = blockIdx.x / ctas, r0 = blockIdx.y * kRanks;
-    const int pad_rank = p.pad_rank, ranks = p.n_parts * pad_rank;
-    const Workspace ws = views(p.h, p.items.n);
+__device__ __forceinline__ Found find(const AdapterParams& p, int index, HShared<kRankTiles, kItemRows>& sh) {
     const int window = p.items.windows == 1 ? 0 : index / p.items.per_window, m0 = window * p.items.window, n = min(p.items.window, p.M - m0);
-    grid_dependency_wait();
-    grid_launch_dependents();
-    if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
     const int nth = index - window * p.items.per_window;
     if (p.n_slots > kSortedSlots || p.M <= 32) find_item_of_32<kItemRows>(p, m0, n, nth, sh.find);
     else find_item<kItemRows>(p, m0, n, nth, sh.find);
-    const int slot = sh.find.slot, rows = sh.find.rows;
-    const int rank = rows == 0 || slot < 0 || slot >= p.n_slots ? 0 : p.ranks ? min(max(p.ranks[slot], 0), p.max_rank) : p.max_rank;
-    // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
-    const int steps = rank > 0 ? p.K / 32 : 0, k0 = steps * cta / ctas * 32, k1 = steps * (cta + 1) / ctas * 32;
+    Found f{sh.find.slot, sh.find.rows, 0};
+    if (static_cast<int>(threadIdx.x) < f.rows) sh.row[threadIdx.x] = sh.find.row[threadIdx.x];
+    if (f.rows > 0 && f.slot >= 0 && f.slot < p.n_slots) f.rank = p.ranks ? min(max(p.ranks[f.slot], 0), p.max_rank) : p.max_rank;
+    __syncthreads();   // (the ring takes the table's memory)
+    return f;
+}
+__device__ __forceinline__ int part_of(int f, int pad_rank) { return (f >= pad_rank) + (f >= 2 * pad_rank) + (f >= 3 * pad_rank); }
+
+// Sums of the warps over this CTA's share of K, for ranks r0 .. (of all parts, padded), left in sh.part.
+template <int kRankTiles, int kItemRows>
+__device__ __forceinline__ void sum_h(const AdapterParams& p, const Found& item, int r0, int cta, int ctas, HShared<kRankTiles, kItemRows>& sh) {
+    using Shared = HShared<kRankTiles, kItemRows>;
+    constexpr int kRows = Shared::kRows, kStageK = Shared::kStageK, kStages = Shared::kStages, kRowBytes = Shared::kRowBytes;
+    constexpr int kTiles = Shared::kTiles, kWarpsK = Shared::kWarpsK;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int steps = item.rank > 0 ? p.K / 32 : 0, k0 = steps * cta / ctas * 32, k1 = steps * (cta + 1) / ctas * 32;
     const int stages = (k1 - k0 + kStageK - 1) / kStageK;
-    auto part_of = [&](int f) { return (f >= pad_rank) + (f >= 2 * pad_rank) + (f >= 3 * pad_rank); };
     // a thread has the same 16 bytes of every kAtOnce-th row in each stage
     constexpr int kPieces = kStageK / 8, kAtOnce = kHThreads / kPieces, kMine = (kRows + kAtOnce - 1) / kAtOnce;
     const int piece = threadIdx.x % kPieces, my_row = threadIdx.x / kPieces;
     const uint16_t* from[kMine];   // null: no such row
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-        const int r = my_row + i * kAtOnce, f = r0 + r - kItemRows, part = part_of(f), k = f - part * pad_rank;
+        const int r = my_row + i * kAtOnce, f = r0 + r - kItemRows, part = part_of(f, p.pad_rank), k = f - part * p.pad_rank;
         from[i] = nullptr;
         if (r < kItemRows) {
-            if (r < rows) from[i] = p.x + sh.find.row[r] * p.ldx + k0 + 8 * piece;
-        } else if (r < kRows && f < ranks && k < rank) {
-            from[i] = p.A + ((static_cast<long long>(slot) * p.n_parts + part) * p.max_rank + k) * p.K + k0 + 8 * piece;
+            if (r < item.rows) from[i] = p.x + sh.row[r] * p.ldx + k0 + 8 * piece;
+        } else if (r < kRows && part < p.n_parts && k < item.rank) {
+            from[i] = p.A + ((static_cast<long long>(item.slot) * p.n_parts + part) * p.max_rank + k) * p.K + k0 + 8 * piece;
         }
     }
-    if (static_cast<int>(threadIdx.x) < rows) {
-        const int m = sh.find.row[threadIdx.x];
-        sh.row[threadIdx.x] = m;
-        if (cta == 0 && blockIdx.y == 0) ws.items[index].row[threadIdx.x] = m;
-    }
-    if (cta == 0 && blockIdx.y == 0 && threadIdx.x == 0) *reinterpret_cast<int4*>(&ws.items[index]) = make_int4(slot, rows, rank, 0);
-    __syncthreads();   // (the ring takes the table's memory)
     const uint32_t to = smem_u32(sh.ring[0][0]) + my_row * kRowBytes + 16 * piece;
     auto ask = [&](int stage, int place) {
         if (stage < stages && k0 + stage * kStageK + 8 * piece < k1) {
@@ -311,11 +304,10 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_h_kernel(const __grid_c
         __syncthreads();   // this stage is there for all, and the one before it has been read
         ask(s + kStages - 1, place == 0 ? kStages - 1 : place - 1);
         const int here = min(kStageK, k1 - k0 - s * kStageK);
-        if (tile * 16 < rows) {
+        if (tile * 16 < item.rows) {
             const uint8_t* at = sh.ring[place][0] + 16 * q;
 #pragma unroll
-            for (int c = 0; c < kStageK / 32 / kWarpsK; ++c) {
-                const int k = 32 * (c * kWarpsK + kw);   // (what ranks and rows that do not exist leave there reaches no sum that is read)
+            for (int k = 32 * kw; k < kStageK; k += 32 * kWarpsK) {   // (what ranks and rows that do not exist leave there reaches no sum that is read)
                 if (k >= here) break;
                 const uint4 va = *reinterpret_cast<const uint4*>(at + (16 * tile + g) * kRowBytes + 2 * k);
                 const uint4 vb = *reinterpret_cast<const uint4*>(at + (16 * tile + 8 + g) * kRowBytes + 2 * k);
@@ -331,8 +323,7 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_h_kernel(const __grid_c
     }
     copies_wait<0>();
     __syncthreads();
-    // sums of the CTA, then those of the cluster, a share of them in each CTA; scaled, and split in two terms
-    if (tile * 16 < rows) {
+    if (tile * 16 < item.rows) {
 #pragma unroll
         for (int t = 0; t < kRankTiles; ++t)
 #pragma unroll
@@ -340,21 +331,61 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_h_kernel(const __grid_c
                 *reinterpret_cast<float2*>(&sh.part[kw][16 * tile + 8 * k + g][8 * t + 2 * q]) = make_float2(acc[t][2 * k], acc[t][2 * k + 1]);
     }
     __syncthreads();
-    const int quads = (rank > 0 ? rows : 0) * (kRanks / 4), share = (quads + ctas - 1) / ctas;   // sums of four ranks of a row; a CTA's share of them
+}
+// The CTA's sum of ranks j .. j + 3 of row m.
+template <class Shared>
+__device__ __forceinline__ float4 cta_sum(const Shared& sh, int m, int j) {
+    float4 sum = *reinterpret_cast<const float4*>(&sh.part[0][m][j]);
+#pragma unroll
+    for (int k = 1; k < Shared::kWarpsK; ++k) {
+        const float4 u = *reinterpret_cast<const float4*>(&sh.part[k][m][j]);
+        sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+    }
+    return sum;
+}
+// Four sums, of ranks r .. r + 3 of a part, scaled and split in two terms; nothing behind the adapter's rank.
+__device__ __forceinline__ uint4 two_terms(float4 sum, float scale, int r, int rank) {
+    const float v[4] = {r < rank ? sum.x * scale : 0.0f, r + 1 < rank ? sum.y * scale : 0.0f, r + 2 < rank ? sum.z * scale : 0.0f, r + 3 < rank ? sum.w * scale : 0.0f};
+    uint4 h;
+    h.x = pack_bf16(v[0], v[1]);
+    h.y = pack_bf16(v[2], v[3]);
+    h.z = pack_bf16(v[0] - bf16_lo(h.x), v[1] - bf16_hi(h.x));
+    h.w = pack_bf16(v[2] - bf16_lo(h.y), v[3] - bf16_hi(h.y));
+    return h;
+}
+
+// Many rows: h of an item goes to the workspace, for the second launch.
+template <int kRankTiles>
+struct ManyHShared : HShared<kRankTiles, kManyRows> {
+    float4 got[kManyRows * 8 * kRankTiles / 4 + 8];   // sums of the cluster's CTAs for this CTA's share of them, one CTA behind the other
+};
+template <int kRankTiles>
+__global__ void __launch_bounds__(kHThreads, 1) adapters_many_h_kernel(const __grid_constant__ AdapterParams p) {
+    using Shared = ManyHShared<kRankTiles>;
+    constexpr int kRanks = Shared::kRanks;
+    extern __shared__ __align__(128) uint8_t smem[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    const int ctas = p.cluster, cta = cluster_ctarank(), index = blockIdx.x / ctas, r0 = blockIdx.y * kRanks, ranks = p.n_parts * p.pad_rank;
+    const Workspace ws = views(p.h, p.items.n);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
+    const Found item = find<kRankTiles, kManyRows>(p, index, sh);
+    if (cta == 0 && blockIdx.y == 0) {
+        if (static_cast<int>(threadIdx.x) < item.rows) ws.items[index].row[threadIdx.x] = sh.row[threadIdx.x];
+        if (threadIdx.x == 0) *reinterpret_cast<int4*>(&ws.items[index]) = make_int4(item.slot, item.rows, item.rank, 0);
+    }
+    // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
+    sum_h<kRankTiles, kManyRows>(p, item, r0, cta, ctas, sh);
+    // the cluster's sums: a share of them in each CTA
+    const int quads = (item.rank > 0 ? item.rows : 0) * (kRanks / 4), share = (quads + ctas - 1) / ctas;
     const float to_share = share > 0 ? 1.0f / share : 0.0f;
     if (ctas > 1) cluster_wait();
     for (int i = threadIdx.x; i < quads; i += kHThreads) {
-        const int m = i / (kRanks / 4), j = i % (kRanks / 4) * 4;
-        float4 sum = *reinterpret_cast<const float4*>(&sh.part[0][m][j]);
-#pragma unroll
-        for (int k = 1; k < kWarpsK; ++k) {
-            const float4 u = *reinterpret_cast<const float4*>(&sh.part[k][m][j]);
-            sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
-        }
         const int c = __float2int_rd((i + 0.5f) * to_share);   // i / share (i + 0.5 is 2^-13 of itself and more away from a border)
-        st_cluster(cluster_map(smem_u32(&sh.got[cta * share + i - c * share]), c), sum);
+        st_cluster(cluster_map(smem_u32(&sh.got[cta * share + i - c * share]), c), cta_sum(sh, i / (kRanks / 4), i % (kRanks / 4) * 4));
     }
-    const float scale = rank > 0 && p.scale ? p.scale[slot] : 1.0f;
+    const float scale = item.rank > 0 && p.scale ? p.scale[item.slot] : 1.0f;
     if (ctas > 1) {
         cluster_arrive();
         cluster_wait();
@@ -363,25 +394,19 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_h_kernel(const __grid_c
     }
     const int i0 = min(quads, share * cta), mine = min(quads, i0 + share) - i0;
     for (int i = threadIdx.x; i < mine; i += kHThreads) {
-        const int m = (i0 + i) / (kRanks / 4), f = r0 + (i0 + i) % (kRanks / 4) * 4, r = f - part_of(f) * pad_rank;
+        const int m = (i0 + i) / (kRanks / 4), f = r0 + (i0 + i) % (kRanks / 4) * 4;
         if (f >= ranks) continue;
         float4 sum = sh.got[i];
         for (int k = 1; k < ctas; ++k) {
             const float4 u = sh.got[k * share + i];
             sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
         }
-        const float v[4] = {r < rank ? sum.x * scale : 0.0f, r + 1 < rank ? sum.y * scale : 0.0f, r + 2 < rank ? sum.z * scale : 0.0f, r + 3 < rank ? sum.w * scale : 0.0f};
-        uint4 h;
-        h.x = pack_bf16(v[0], v[1]);
-        h.y = pack_bf16(v[2], v[3]);
-        h.z = pack_bf16(v[0] - bf16_lo(h.x), v[1] - bf16_hi(h.x));
-        h.w = pack_bf16(v[2] - bf16_lo(h.y), v[3] - bf16_hi(h.y));
-        ws.h[static_cast<long long>(sh.row[m]) * (ranks / 4) + f / 4] = h;
+        ws.h[static_cast<long long>(sh.row[m]) * (ranks / 4) + f / 4] = two_terms(sum, scale, f - part_of(f, p.pad_rank) * p.pad_rank, item.rank);
     }
 }
 
 // ---------------------------------------------------------------- y
-// In both kernels a lane has eight columns that follow one another: column 2 q + e of the j-th 8-column fragment stands for column 8 q + 2 j + e
+// In both forms a lane has eight columns that follow one another: column 2 q + e of the j-th 8-column fragment stands for column 8 q + 2 j + e
 // of a block of 32.  bf16: the accumulators begin with base (their sum is cut to 24 bits, and then rounded to 8); fp32: base is added to
 // the sum.  What lies behind an adapter's rank may be anything: `masked` clears it in a lane's four ranks of B.
 __device__ __forceinline__ uint2 masked(uint2 b, int left) {
@@ -456,78 +481,118 @@ __device__ __forceinline__ void copy_rows(const AdapterParams& p, const int* row
     }
 }
 
-// Few rows: an item of up to 16 rows and 64 columns per warp, everything straight from memory.
-constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32;
-template <class T>
-__global__ void __launch_bounds__(kFewThreads, 4) adapters_few_y_kernel(const __grid_constant__ AdapterParams p, int units) {
-    const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int pad_rank = p.pad_rank, quads = p.n_parts * pad_rank / 4;
-    const Workspace ws = views(p.h, p.items.n);
-    const int ctas = (units + kFewWarps - 1) / kFewWarps, index = blockIdx.x / ctas, unit = (blockIdx.x - index * ctas) * kFewWarps + (threadIdx.x >> 5);
-    const Unit at = unit_of(p, unit, 64);
-    const Item& item = ws.items[index];
+// Few rows: one launch.  Every CTA of an item's cluster gets all of its sums, and a share of the columns: 64 per warp, straight from memory.
+template <int kRankTiles>
+struct FewShared : HShared<kRankTiles, kFewRows> {
+    uint4 h[kFewRows * PRQ_MULTI_MAX * PRQ_ADAPTER_MAX_RANK / 4];   // [rank / 4][row]
+    float4 got[8][kFewRows * 8 * kRankTiles / 4];                    // from each CTA of the cluster
+};
+template <class T, int kRankTiles>
+__global__ void __launch_bounds__(kHThreads, 1) adapters_few_kernel(const __grid_constant__ AdapterParams p, int passes, int units) {
+    using Shared = FewShared<kRankTiles>;
+    constexpr int kRanks = Shared::kRanks;
+    extern __shared__ __align__(128) uint8_t smem[];
+    Shared& sh = *reinterpret_cast<Shared*>(smem);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+    const int ctas = p.cluster, cta = cluster_ctarank(), index = blockIdx.x / ctas, pad_rank = p.pad_rank, ranks = p.n_parts * pad_rank;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int4 head = *reinterpret_cast<const int4*>(&item);
-    int row[2] = {item.row[g], item.row[8 + g]};
-    const int other = item.row[0];
-    const int slot = head.x, rows = head.y, rank = head.z;
-    if (unit >= units || rows == 0) return;
-    if (rank == 0) {
-        if (p.base != p.y) copy_rows<T>(p, item.row, rows, at.n0, min(at.end, at.n0 + 64), lane, 32);
-        return;
+    if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
+    const Found item = find<kRankTiles, kFewRows>(p, index, sh);
+    const int rows = item.rows, rank = item.rank, stride = ctas * kHWarps;
+    if (rank > 0 && lane == 0) {
+        // the first columns' share of B is on its way into L2 meanwhile
+        const Unit at = unit_of(p, cta * kHWarps + warp, 64);
+        if (at.n0 < at.end) prefetch_l2(p.B + (static_cast<long long>(item.slot) * p.N + at.n0) * p.max_rank, min(64, at.end - at.n0) * p.max_rank * 2);
     }
-    // (lanes whose row does not exist repeat the item's first one up to the store)
+    const float scale = rank > 0 && p.scale ? p.scale[item.slot] : 1.0f;
+    const int quads = rank > 0 ? rows * (kRanks / 4) : 0;
+    // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
+    for (int pass = 0; pass < passes; ++pass) {
+        sum_h<kRankTiles, kFewRows>(p, item, pass * kRanks, cta, ctas, sh);
+        if (ctas > 1) cluster_wait();
+        for (int i = threadIdx.x; i < quads; i += kHThreads) {
+            const float4 sum = cta_sum(sh, i / (kRanks / 4), i % (kRanks / 4) * 4);
+            for (int c = 0; c < ctas; ++c) st_cluster(cluster_map(smem_u32(&sh.got[cta][i]), c), sum);
+        }
+        if (ctas > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        for (int i = threadIdx.x; i < quads; i += kHThreads) {
+            const int m = i / (kRanks / 4), f = pass * kRanks + i % (kRanks / 4) * 4;
+            if (f >= ranks) continue;
+            float4 sum = sh.got[0][i];
+            for (int c = 1; c < ctas; ++c) {
+                const float4 u = sh.got[c][i];
+                sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+            }
+            sh.h[f / 4 * kFewRows + m] = two_terms(sum, scale, f - part_of(f, pad_rank) * pad_rank, rank);
+        }
+        __syncthreads();
+        if (ctas > 1 && pass + 1 < passes) cluster_arrive();   // (what was got has been read)
+    }
+
     const bool mine[2] = {g < rows, 8 + g < rows};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) row[i] = mine[i] ? row[i] : other;
-    Columns<T> v[2][2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int col = at.n0 + 32 * j + 8 * q;
-            v[i][j] = Columns<T>{};
-            if (mine[i] && col + 8 <= at.end) v[i][j].load(static_cast<const T*>(p.base) + row[i] * p.ldbase + col);
-        }
-    float acc[2][4][4];
-    const uint16_t* B = p.B + (static_cast<long long>(slot) * p.N + at.n0 + 8 * (g >> 1) + (g & 1)) * p.max_rank + 4 * q;
-    const uint4* H = ws.h + at.part * (pad_rank / 4) + q;
-    const int n_left = at.end - at.n0 - 8 * (g >> 1) - (g & 1);   // columns of this lane's row of B up to the end
+    // (lanes whose row does not exist repeat the item's first one up to the store)
+    const long long row[2] = {mine[0] ? sh.row[g] : 0, mine[1] ? sh.row[8 + g] : 0};
 #pragma unroll 1
-    for (int k = 0; k < rank; k += 16) {
-        const int left = rank - k - 4 * q;
-        uint2 b[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int n = 32 * (j / 4) + 2 * (j % 4);
-            b[j] = make_uint2(0, 0);
-            if (n < n_left && left > 0) b[j] = *reinterpret_cast<const uint2*>(B + static_cast<long long>(n) * p.max_rank + k);
+    for (int unit = cta * kHWarps + warp; unit < units && rows > 0; unit += stride) {
+        const Unit at = unit_of(p, unit, 64);
+        if (rank == 0) {
+            if (p.base != p.y) copy_rows<T>(p, sh.row, rows, at.n0, min(at.end, at.n0 + 64), lane, 32);
+            continue;
         }
-        const uint4 ha = H[static_cast<long long>(row[0]) * quads + k / 4], hb = H[static_cast<long long>(row[1]) * quads + k / 4];
-        if (k == 0) {
+        Columns<T> v[2][2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int i = 0; i < 2; ++i) begin_sum<T>(acc[j], v[i][j], 2 * i);
+            for (int j = 0; j < 2; ++j) {
+                const int col = at.n0 + 32 * j + 8 * q;
+                v[i][j] = Columns<T>{};
+                if (mine[i] && col + 8 <= at.end) v[i][j].load(static_cast<const T*>(p.base) + row[i] * p.ldbase + col);
+            }
+        float acc[2][4][4];
+        const uint16_t* B = p.B + (static_cast<long long>(item.slot) * p.N + at.n0 + 8 * (g >> 1) + (g & 1)) * p.max_rank + 4 * q;
+        const uint4* H = sh.h + (at.part * (pad_rank / 4) + q) * kFewRows + g;
+        const int n_left = at.end - at.n0 - 8 * (g >> 1) - (g & 1);   // columns of this lane's row of B up to the end
+#pragma unroll 1
+        for (int k = 0; k < rank; k += 16) {
+            const int left = rank - k - 4 * q;
+            uint2 b[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int n = 32 * (j / 4) + 2 * (j % 4);
+                b[j] = make_uint2(0, 0);
+                if (n < n_left && left > 0) b[j] = *reinterpret_cast<const uint2*>(B + static_cast<long long>(n) * p.max_rank + k);
+            }
+            const uint4 ha = H[k / 4 * kFewRows], hb = H[k / 4 * kFewRows + 8];   // (of a row that does not exist: reaches no sum that is stored)
+            if (k == 0) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) begin_sum<T>(acc[j], v[i][j], 2 * i);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (left < 4) b[j] = masked(b[j], left);
+                mma_bf16(acc[j / 4][j % 4], ha.x, hb.x, ha.y, hb.y, b[j].x, b[j].y);
+                mma_bf16(acc[j / 4][j % 4], ha.z, hb.z, ha.w, hb.w, b[j].x, b[j].y);
+            }
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if (left < 4) b[j] = masked(b[j], left);
-            mma_bf16(acc[j / 4][j % 4], ha.x, hb.x, ha.y, hb.y, b[j].x, b[j].y);
-            mma_bf16(acc[j / 4][j % 4], ha.z, hb.z, ha.w, hb.w, b[j].x, b[j].y);
-        }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int col = at.n0 + 32 * j + 8 * q, cols = at.end - col;
+                if (!mine[i] || cols <= 0) continue;
+                T* to = static_cast<T*>(p.y) + row[i] * p.ldy + col;
+                if (cols >= 8) end_sum<T>(acc[j], v[i][j], 2 * i).store(to);
+                else add_last<T>(acc[j], 2 * i, cols, static_cast<const T*>(p.base) + row[i] * p.ldbase + col, to);
+            }
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int col = at.n0 + 32 * j + 8 * q, cols = at.end - col;
-            if (!mine[i] || cols <= 0) continue;
-            T* to = static_cast<T*>(p.y) + row[i] * p.ldy + col;
-            if (cols >= 8) end_sum<T>(acc[j], v[i][j], 2 * i).store(to);
-            else add_last<T>(acc[j], 2 * i, cols, static_cast<const T*>(p.base) + row[i] * p.ldbase + col, to);
-        }
 }
 
 // Many rows: a CTA has an item and `span` tiles of kCols columns of one part.  Tiles of base and B come into a ring in shared memory; a
@@ -693,44 +758,66 @@ cudaError_t launch_kernel(void (*kernel)(Params...), dim3 blocks, int threads, i
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <int kRankTiles, int kItemRows>
-cudaError_t launch_h(const AdapterParams& p, int passes, cudaStream_t stream) {
-    static OncePerDevice once;
-    constexpr int kBytes = sizeof(HShared<kRankTiles, kItemRows>);
-    static_assert(kBytes <= 227 * 1024, "shared memory");
-    const auto kernel = adapters_h_kernel<kRankTiles, kItemRows>;
-    const cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes); });
-    if (e != cudaSuccess) return e;
-    return launch_kernel(kernel, dim3(p.items.n * p.cluster, passes), kHThreads, p.cluster, kBytes, stream, p);
+// Lets a kernel use `bytes` of dynamic shared memory, once per device.
+template <class Kernel>
+cudaError_t allow_shared(OncePerDevice& once, Kernel kernel, size_t bytes) {
+    return once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)); });
 }
-template <int kItemRows>
-cudaError_t launch_h(const AdapterParams& p, cudaStream_t stream) {
+struct Passes { int passes, tiles; };   // all ranks, eight at a time, in passes of up to 64
+Passes passes_of(const AdapterParams& p) {
     const int ranks = p.n_parts * p.pad_rank, passes = (ranks + 63) / 64, tiles = (ranks / 8 + passes - 1) / passes;
-    return tiles <= 2 ? launch_h<2, kItemRows>(p, passes, stream) : tiles <= 4 ? launch_h<4, kItemRows>(p, passes, stream)
-         : tiles <= 6 ? launch_h<6, kItemRows>(p, passes, stream) : launch_h<8, kItemRows>(p, passes, stream);
+    return Passes{passes, tiles <= 2 ? 2 : tiles <= 4 ? 4 : tiles <= 6 ? 6 : 8};
+}
+template <class F>
+cudaError_t with_tiles(int tiles, F&& f) {
+    return tiles == 2 ? f(std::integral_constant<int, 2>()) : tiles == 4 ? f(std::integral_constant<int, 4>())
+         : tiles == 6 ? f(std::integral_constant<int, 6>()) : f(std::integral_constant<int, 8>());
 }
 template <class T, int kSteps16>
 cudaError_t launch_many_y(const AdapterParams& p, int units, int span, cudaStream_t stream) {
     static OncePerDevice once;
     const auto kernel = adapters_many_y_kernel<T, kSteps16>;
-    const cudaError_t e = once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kManyStages * many_stage_bytes<T>(PRQ_ADAPTER_MAX_RANK)); });
+    const cudaError_t e = allow_shared(once, kernel, kManyStages * many_stage_bytes<T>(PRQ_ADAPTER_MAX_RANK));
     if (e != cudaSuccess) return e;
     return launch_kernel(kernel, dim3(units * p.items.n), kManyThreads, 1, kManyStages * many_stage_bytes<T>(p.max_rank), stream, p, units, span);
 }
+// Pieces of `width` columns of all parts.
+int pieces_of(const AdapterParams& p, int width) {
+    int n = 0;
+    for (int i = 0; i < p.n_parts; ++i) n += (p.part_end[i] - (i ? p.part_end[i - 1] : 0) + width - 1) / width;
+    return n;
+}
 template <class T>
-cudaError_t launch_y(const AdapterParams& p, int num_sms, cudaStream_t stream) {
-    const bool few = p.M <= kFewCall;
-    int span = 1;
-    if (!few) {
-        span = 4;
-        if (const char* v = dev_knobs_enabled() ? std::getenv("PRQ_AD_PER") : nullptr) span = atoi(v);
-    }
-    const int width = few ? 64 : kManyCols<T> * span;
-    int units = 0;
-    for (int i = 0; i < p.n_parts; ++i) units += (p.part_end[i] - (i ? p.part_end[i - 1] : 0) + width - 1) / width;
+cudaError_t launch_few(const AdapterParams& p, cudaStream_t stream) {
+    const Passes t = passes_of(p);
+    return with_tiles(t.tiles, [&](auto tiles) {
+        static OncePerDevice once;
+        using Shared = FewShared<decltype(tiles)::value>;
+        static_assert(sizeof(Shared) <= 227 * 1024, "shared memory");
+        const auto kernel = adapters_few_kernel<T, decltype(tiles)::value>;
+        const cudaError_t e = allow_shared(once, kernel, sizeof(Shared));
+        if (e != cudaSuccess) return e;
+        return launch_kernel(kernel, dim3(p.items.n * p.cluster), kHThreads, p.cluster, sizeof(Shared), stream, p, t.passes, pieces_of(p, 64));
+    });
+}
+cudaError_t launch_many_h(const AdapterParams& p, cudaStream_t stream) {
+    const Passes t = passes_of(p);
+    return with_tiles(t.tiles, [&](auto tiles) {
+        static OncePerDevice once;
+        using Shared = ManyHShared<decltype(tiles)::value>;
+        static_assert(sizeof(Shared) <= 227 * 1024, "shared memory");
+        const auto kernel = adapters_many_h_kernel<decltype(tiles)::value>;
+        const cudaError_t e = allow_shared(once, kernel, sizeof(Shared));
+        if (e != cudaSuccess) return e;
+        return launch_kernel(kernel, dim3(p.items.n * p.cluster, t.passes), kHThreads, p.cluster, sizeof(Shared), stream, p);
+    });
+}
+template <class T>
+cudaError_t launch_many_y(const AdapterParams& p, cudaStream_t stream) {
+    int span = 4;
+    if (const char* v = dev_knobs_enabled() ? std::getenv("PRQ_AD_PER") : nullptr) span = atoi(v);
+    const int units = pieces_of(p, kManyCols<T> * span), steps = p.pad_rank / 16;
     if (static_cast<long long>(units) * p.items.n > 0x7fffffffll) return cudaErrorInvalidValue;
-    if (few) return launch_kernel(adapters_few_y_kernel<T>, dim3((units + kFewWarps - 1) / kFewWarps * p.items.n), kFewThreads, 1, 0, stream, p, units);
-    const int steps = p.pad_rank / 16;
     return steps == 1 ? launch_many_y<T, 1>(p, units, span, stream) : steps == 2 ? launch_many_y<T, 2>(p, units, span, stream)
          : steps <= 4 ? launch_many_y<T, 4>(p, units, span, stream) : launch_many_y<T, 8>(p, units, span, stream);
 }
@@ -739,6 +826,7 @@ cudaError_t launch_y(const AdapterParams& p, int num_sms, cudaStream_t stream) {
 
 size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank) {
     const AdapterItems items = plan_items(M, n_slots);
+    if (M <= kFewCall) return 0;
     const size_t ranks = n_parts * ((max_rank + 15) & ~15);
     return items.n < 0 ? 0 : sizeof(Item) * items.n + 4 * ranks * static_cast<size_t>(M);
 }
@@ -749,18 +837,23 @@ cudaError_t launch_adapters(const AdapterParams& in, bool bf16, int num_sms, cud
     p.pad_rank = (p.max_rank + 15) & ~15;
     if (p.items.n < 1) return cudaErrorInvalidValue;
     const bool few = p.M <= kFewCall;
-    const int passes = (p.n_parts * p.pad_rank + 63) / 64;
+    const int passes = few ? 1 : passes_of(p).passes;
     const int full = p.M / kManyRows, items = few ? p.items.n : full + std::min(p.n_slots, full) / 4 + 1;
     p.cluster = 1;
     for (int c = 2; c <= 8; ++c)
         if (static_cast<long long>(items) * passes * c <= num_sms / 18 * (18 / c) * c && p.K / 32 >= (few ? 8 : 4) * c) p.cluster = c;
     if (const char* v = dev_knobs_enabled() ? std::getenv("PRQ_AD_CLUSTER") : nullptr) p.cluster = atoi(v);
-    const cudaError_t e = few ? launch_h<kFewRows>(p, stream) : launch_h<kManyRows>(p, stream);
+    if (few) {
+        const cudaError_t e = bf16 ? launch_few<__nv_bfloat16>(p, stream) : launch_few<float>(p, stream);
+        *launches = e == cudaSuccess;
+        return e;
+    }
+    cudaError_t e = launch_many_h(p, stream);
     if (e != cudaSuccess) return e;
     ++*launches;
-    const cudaError_t e2 = bf16 ? launch_y<__nv_bfloat16>(p, num_sms, stream) : launch_y<float>(p, num_sms, stream);
-    if (e2 == cudaSuccess) ++*launches;
-    return e2;
+    e = bf16 ? launch_many_y<__nv_bfloat16>(p, stream) : launch_many_y<float>(p, stream);
+    if (e == cudaSuccess) ++*launches;
+    return e;
 }
 
 }  // namespace prq
