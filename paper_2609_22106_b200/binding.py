@@ -545,20 +545,21 @@ def _require(ok: bool, where: str):
         raise PrqError(1, where)
 
 
-_current_device = None
+# Names that the calls below look up (torch is imported with the first of them; a call on a few rows takes the GPU less time than
+# Python's part of it takes the host).
+_torch = _f32 = _bf16 = _i32 = _current_device = None
 
 
-def _on_current_device(*tensors) -> bool:
-    global _current_device
-    if _current_device is None:
-        import torch
+def _load_torch():
+    global _torch, _f32, _bf16, _i32, _current_device
+    import torch
 
-        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    dev = _current_device()
-    return all(t is None or t.get_device() == dev for t in tensors)
+    _torch, _f32, _bf16, _i32 = torch, torch.float32, torch.bfloat16, torch.int32
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 ADAPTER_MAX_RANK = 128
+ADAPTER_FEW_ROWS = 128   # rows of a call that needs no workspace
 
 
 class AdapterPool(ctypes.Structure):
@@ -584,6 +585,7 @@ class Adapters:
             _require(t is None or (t.dtype == dtype and tuple(t.shape) == (S,) and t.is_contiguous()), where)
         _require(all(t is None or t.get_device() == A.get_device() for t in (B, scale, ranks)) and A.is_cuda, where)
         self.A, self.B, self.scale, self.ranks, self.parts, self.N, self.K = A, B, scale, ranks, parts, sum(parts), K
+        self.device = A.get_device()
         self._pool = AdapterPool(ctypes.sizeof(AdapterPool), S, R, K, P, (ctypes.c_int * 4)(*parts), _dptr(A), _dptr(B), _dptr(scale), _dptr(ranks))
         self._p = ctypes.addressof(self._pool)
 
@@ -598,26 +600,40 @@ def adapters_workspace(adapters: Adapters, M: int):
 def linear_adapters(adapters: Adapters, x, row_adapter, base, out=None, workspace=None, stream=None):
     """base + scale * (x A^T) B^T with the adapter that row_adapter (int32 (M,), -1: none) names for each row.  x: bf16 (M, K); base: the
     projection's output, fp32 or bf16 (M, N).  Adds in place unless `out` is given; returns the result."""
-    import torch
-
-    M, out = x.shape[0], base if out is None else out
-    _require(x.dtype == torch.bfloat16 and row_adapter.dtype == torch.int32 and base.dtype == out.dtype and base.dtype in (torch.float32, torch.bfloat16) and
-             tuple(x.shape) == (M, adapters.K) and tuple(row_adapter.shape) == (M,) and tuple(base.shape) == tuple(out.shape) == (M, adapters.N), "linear_adapters")
+    if _torch is None:
+        _load_torch()
+    where = "linear_adapters"
+    M, K = x.shape
+    N, dtype = adapters.N, base.dtype
+    if out is None:
+        out = base
+    elif not (out.dtype is dtype and out.shape == base.shape):
+        _require(False, where)
+    if not (K == adapters.K and x.dtype is _bf16 and row_adapter.dtype is _i32 and row_adapter.shape == (M,) and base.shape == (M, N) and
+            (dtype is _bf16 or dtype is _f32)):
+        _require(False, where)
     if M == 0:
         return out
-    _require((x.stride(1) == 1) and row_adapter.is_contiguous() and (adapters.N == 1 or base.stride(1) == out.stride(1) == 1) and
-             _on_current_device(x, row_adapter, base, out, workspace, adapters.A), "linear_adapters")
+    (ldx, one), (ldbase, b1), (ldout, o1) = x.stride(), base.stride(), out.stride()
+    device = _current_device()
+    if not (one == 1 and (N == 1 or b1 == o1 == 1) and row_adapter.is_contiguous() and
+            x.get_device() == row_adapter.get_device() == base.get_device() == out.get_device() == adapters.device == device):
+        _require(False, where)
+    if M == 1:   # a single row has no stride
+        ldx, ldbase = K, (N + 7) // 8 * 8
+        ldout = ldbase
     if workspace is None:
-        if stream is None:
-            workspace = adapters_workspace(adapters, M)
-        else:   # from the memory of the call's stream
-            with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream, device=x.device)):
+        if M > ADAPTER_FEW_ROWS:
+            if stream is None:
                 workspace = adapters_workspace(adapters, M)
-    one = M == 1   # a single row has no stride
-    _check(lib().prq_linear_adapters(adapters._p, _dptr(row_adapter), _dptr(x), M, adapters.K if one else x.stride(0), _dptr(base),
-                                     (adapters.N + 7) // 8 * 8 if one else base.stride(0), _dptr(out), (adapters.N + 7) // 8 * 8 if one else out.stride(0),
-                                     F32 if base.dtype == torch.float32 else BF16, _dptr(workspace), workspace.numel() * workspace.element_size(),
-                                     _stream_ptr(stream)), "prq_linear_adapters")
+            else:   # from the memory of the call's stream
+                with _torch.cuda.stream(stream if isinstance(stream, _torch.cuda.Stream) else _torch.cuda.ExternalStream(stream.cuda_stream, device=x.device)):
+                    workspace = adapters_workspace(adapters, M)
+    elif workspace.get_device() != device:
+        _require(False, where)
+    _check(lib().prq_linear_adapters(adapters._p, row_adapter.data_ptr(), x.data_ptr(), M, ldx, base.data_ptr(), ldbase, out.data_ptr(), ldout,
+                                     BF16 if dtype is _bf16 else F32, None if workspace is None else workspace.data_ptr(),
+                                     0 if workspace is None else workspace.nbytes, _stream_ptr(stream)), "prq_linear_adapters")
     return out
 
 
@@ -675,40 +691,51 @@ class Rope:
 _HEADS = struct.Struct("@PPqqqqiP")   # prq_heads, in native alignment
 
 
-def _heads(t, to, weight, M: int, D: int, dtype, where: str):
+def _heads(t, to, weight, M: int, D: int, dtype, device: int, where: str):
     """A prq_heads of a tensor (M, heads, D) and where its result goes."""
-    import torch
+    shape, (ld, hs, one) = t.shape, t.stride()
+    if not (shape[0] == M and shape[2] == D and one == 1 and t.dtype is dtype and t.get_device() == device):
+        _require(False, where)
+    at = t.data_ptr()
+    if to is t:
+        to_at, ldo, hso = at, ld, hs
+    else:
+        ldo, hso, one = to.stride()
+        if not (one == 1 and to.shape == shape and to.dtype is dtype and to.get_device() == device):
+            _require(False, where)
+        to_at = to.data_ptr()
+    if weight is None:
+        return _HEADS.pack(at, to_at, ld, hs, ldo, hso, shape[1], 0)
+    if not (weight.dtype is _f32 and weight.shape == (D,) and weight.is_contiguous() and weight.get_device() == device):
+        _require(False, where)
+    return _HEADS.pack(at, to_at, ld, hs, ldo, hso, shape[1], weight.data_ptr())
 
-    _require(t.dim() == 3 and t.shape[0] == M and t.shape[2] == D and t.shape == to.shape and t.dtype == to.dtype == dtype and
-             (D == 1 or (t.stride(2) == 1 and to.stride(2) == 1)) and _on_current_device(t, to, weight), where)
-    _require(weight is None or (weight.dtype == torch.float32 and tuple(weight.shape) == (D,) and weight.is_contiguous()), where)
-    sx, so = t.stride(), to.stride()
-    return _HEADS.pack(t.data_ptr(), to.data_ptr(), sx[0], sx[1], so[0], so[1], t.shape[1], 0 if weight is None else weight.data_ptr())
 
-
-def _rotate(rope, positions, q, k, weights, eps, out, stream, where):
-    import torch
-
-    to = ((q, k) if out is None else (out, None) if k is None else out)
-    M = positions.shape[0]
-    _require(positions.dtype == torch.int32 and positions.dim() == 1 and (M < 2 or positions.stride(0) == 1) and _on_current_device(positions) and
-             q.dtype in (torch.float32, torch.bfloat16), where)
-    hq = _heads(q, to[0], weights[0], M, rope.head_dim, q.dtype, where)
-    hk = None if k is None else _heads(k, to[1], weights[1], M, rope.head_dim, q.dtype, where)
-    dtype = F32 if q.dtype == torch.float32 else BF16
+def _rotate(rope, positions, q, k, q_weight, k_weight, eps, out, stream, where):
+    if _torch is None:
+        _load_torch()
+    device, dtype, D = _current_device(), q.dtype, rope.head_dim
+    to_q, to_k = (q, k) if out is None else (out, None) if k is None else out
+    M, = positions.shape
+    if not (positions.dtype is _i32 and positions.is_contiguous() and positions.get_device() == device and (dtype is _bf16 or dtype is _f32) and
+            q.dim() == to_q.dim() == 3 and (k is None or k.dim() == to_k.dim() == 3)):
+        _require(False, where)
+    hq = _heads(q, to_q, q_weight, M, D, dtype, device, where)
+    hk = None if k is None else _heads(k, to_k, k_weight, M, D, dtype, device, where)
+    dtype = BF16 if dtype is _bf16 else F32
     if eps is None:
         _check(lib().prq_rotate_heads(rope._h, positions.data_ptr(), M, hq, hk, dtype, _stream_ptr(stream)), where)
     else:
         _check(lib().prq_norm_rotate_heads(rope._h, positions.data_ptr(), M, hq, hk, eps, dtype, _stream_ptr(stream)), where)
-    return to[0] if k is None else to
+    return to_q if k is None else (to_q, to_k) if out is None else out
 
 
 def rotate_heads(rope: Rope, positions, q, k=None, out=None, stream=None):
     """Turns the heads q (M, heads, head_dim) -- and k, in the same launch -- by their rows' positions (int32 (M,); POSITION_NONE: the row is
     left out).  Tensors may be slices of the stacked projection's output.  In place unless out (a pair if k is given) is given."""
-    return _rotate(rope, positions, q, k, (None, None), None, out, stream, "prq_rotate_heads")
+    return _rotate(rope, positions, q, k, None, None, None, out, stream, "prq_rotate_heads")
 
 
 def norm_rotate_heads(rope: Rope, positions, q, k=None, q_weight=None, k_weight=None, eps: float = 1e-6, out=None, stream=None):
     """The RMS norm of every head (weights: fp32 (head_dim,) or None), then rotate_heads, in one pass."""
-    return _rotate(rope, positions, q, k, (q_weight, k_weight), eps, out, stream, "prq_norm_rotate_heads")
+    return _rotate(rope, positions, q, k, q_weight, k_weight, eps, out, stream, "prq_norm_rotate_heads")
