@@ -93,19 +93,21 @@ AdapterItems plan_items(int M, int n_slots) {
     return t;
 }
 
-constexpr int kHThreads = 512, kHWarps = kHThreads / 32, kSteps = kWindow / kHThreads;
+constexpr int kHThreads = 512, kHWarps = kHThreads / 32;
 
 struct FindShared {
     uint16_t count[kHWarps][kSortedSlots + 1];   // rows per warp and adapter (the last one: none), then the rows in front of them
     int warp_items[kHWarps];
-    int slot, first, rows;
+    int slot, first, rows, all, bare;   // all: items of the window; bare: those of them, the last ones, whose rows have no adapter
     int row[kManyRows];
 };
 
-// The CTA's item: the index-th one of the window at m0.  Every thread keeps up to kSteps rows and their places among the rows of
+// The CTA's item: the index-th one of the window at m0.  Every thread keeps up to eight rows and their places among the rows of
 // their adapter (a warp's rows follow one another, so that the order is that of the rows and a prompt's stay together).
 template <int kItemRows>
 __device__ __forceinline__ void find_item(const AdapterParams& p, int m0, int n, int index, FindShared& f) {
+    constexpr int kSteps = kItemRows == kFewRows ? 1 : kWindow / kHThreads;   // (what is executed once counts by its instructions' way here, too)
+    static_assert(kFewCall <= kHThreads, "few rows: one step");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kinds = p.n_slots + 1;
     const int steps = (n + kHThreads - 1) / kHThreads, begin = warp * steps * 32;
     int slot[kSteps], place[kSteps];
@@ -163,6 +165,10 @@ __device__ __forceinline__ void find_item(const AdapterParams& p, int m0, int n,
     int first = sum - items;
 #pragma unroll
     for (int w = 0; w < kHWarps; ++w) first += w < warp ? f.warp_items[w] : 0;
+    if (kind == kinds - 1) {
+        f.all = first + items;
+        f.bare = items;
+    }
     if (index >= first && index < first + items) {
         f.slot = kind;
         f.first = (index - first) * kItemRows;
@@ -181,7 +187,8 @@ __device__ __forceinline__ void find_item(const AdapterParams& p, int m0, int n,
     __syncthreads();
 }
 
-// The same within 32 rows that follow one another, for any number of adapters, by one warp: items in the order of their first rows.
+// The same within 32 rows that follow one another, for any number of adapters, by one warp: items in the order of their first rows, those without an
+// adapter last.
 template <int kItemRows>
 __device__ __forceinline__ void find_item_of_32(const AdapterParams& p, int m0, int n, int index, FindShared& f) {
     if (threadIdx.x < 32) {
@@ -191,10 +198,14 @@ __device__ __forceinline__ void find_item_of_32(const AdapterParams& p, int m0, 
         const unsigned same = __match_any_sync(0xffffffffu, slot), before = (1u << lane) - 1;
         const int nth = __popc(same & before);
         const bool leads = lane < n && nth % kItemRows == 0;
-        const unsigned leaders = __ballot_sync(0xffffffffu, leads);
-        const bool chosen = leads && __popc(leaders & before) == index;
+        const unsigned leaders = __ballot_sync(0xffffffffu, leads), bare = __ballot_sync(0xffffffffu, leads && slot < 0), other = leaders & ~bare;
+        const bool chosen = leads && (slot < 0 ? __popc(other) + __popc(bare & before) : __popc(other & before)) == index;
         const unsigned who = __ballot_sync(0xffffffffu, chosen);
-        if (lane == 0) f.rows = 0;
+        if (lane == 0) {
+            f.rows = 0;
+            f.all = __popc(leaders);
+            f.bare = __popc(bare);
+        }
         __syncwarp();
         if (who) {
             const int first = __shfl_sync(0xffffffffu, nth, __ffs(who) - 1);
@@ -209,15 +220,21 @@ __device__ __forceinline__ void find_item_of_32(const AdapterParams& p, int m0, 
 }
 
 struct Workspace {
+    int* counts;       // items of each window that have something to do: its first ones
     Item* items;
     uint4* h;          // M x ranks / 4: (hi, lo) of four ranks
 };
-__host__ __device__ inline Workspace views(void* at, int n_items) {
-    return Workspace{static_cast<Item*>(at), reinterpret_cast<uint4*>(static_cast<uint8_t*>(at) + sizeof(Item) * n_items)};
+__host__ __device__ inline size_t counts_bytes(const AdapterItems& t) { return (sizeof(int) * t.windows + 15) / 16 * 16; }
+__host__ __device__ inline Workspace views(void* at, const AdapterItems& t) {
+    Item* items = reinterpret_cast<Item*>(static_cast<uint8_t*>(at) + counts_bytes(t));
+    return Workspace{static_cast<int*>(at), items, reinterpret_cast<uint4*>(items + t.n)};
 }
 
 __device__ __forceinline__ void copy16(uint32_t to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t to, const void* from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int n>
@@ -240,7 +257,7 @@ struct HShared {
     };
     int row[kItemRows];
 };
-struct Found { int slot, rows, rank; };
+struct Found { int slot, rows, rank, all, bare; };
 // The cluster's item, its rows in sh.row.
 template <int kRankTiles, int kItemRows>
 __device__ __forceinline__ Found find(const AdapterParams& p, int index, HShared<kRankTiles, kItemRows>& sh) {
@@ -248,7 +265,7 @@ __device__ __forceinline__ Found find(const AdapterParams& p, int index, HShared
     const int nth = index - window * p.items.per_window;
     if (p.n_slots > kSortedSlots || p.M <= 32) find_item_of_32<kItemRows>(p, m0, n, nth, sh.find);
     else find_item<kItemRows>(p, m0, n, nth, sh.find);
-    Found f{sh.find.slot, sh.find.rows, 0};
+    Found f{sh.find.slot, sh.find.rows, 0, sh.find.all, sh.find.bare};
     if (static_cast<int>(threadIdx.x) < f.rows) sh.row[threadIdx.x] = sh.find.row[threadIdx.x];
     if (f.rows > 0 && f.slot >= 0 && f.slot < p.n_slots) f.rank = p.ranks ? min(max(p.ranks[f.slot], 0), p.max_rank) : p.max_rank;
     __syncthreads();   // (the ring takes the table's memory)
@@ -269,16 +286,19 @@ __device__ __forceinline__ void sum_h(const AdapterParams& p, const Found& item,
     constexpr int kPieces = kStageK / 8, kAtOnce = kHThreads / kPieces, kMine = (kRows + kAtOnce - 1) / kAtOnce;
     const int piece = threadIdx.x % kPieces, my_row = threadIdx.x / kPieces;
     const uint16_t* from[kMine];   // null: no such row
+    const uint16_t* A = p.A + static_cast<long long>(item.slot) * p.n_parts * p.max_rank * p.K + k0 + 8 * piece;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-        const int r = my_row + i * kAtOnce, f = r0 + r - kItemRows, part = part_of(f, p.pad_rank), k = f - part * p.pad_rank;
+        const int r = my_row + i * kAtOnce;
         from[i] = nullptr;
-        if (r < kItemRows) {
+        if (i * kAtOnce < kItemRows) {   // (kItemRows is a multiple of kAtOnce)
             if (r < item.rows) from[i] = p.x + sh.row[r] * p.ldx + k0 + 8 * piece;
-        } else if (r < kRows && part < p.n_parts && k < item.rank) {
-            from[i] = p.A + ((static_cast<long long>(item.slot) * p.n_parts + part) * p.max_rank + k) * p.K + k0 + 8 * piece;
+        } else {
+            const int f = r0 + r - kItemRows, part = part_of(f, p.pad_rank), k = f - part * p.pad_rank;
+            if (r < kRows && part < p.n_parts && k < item.rank) from[i] = A + static_cast<long long>(part * p.max_rank + k) * p.K;
         }
     }
+    static_assert(kItemRows % kAtOnce == 0, "rows of x and of A in different turns");
     const uint32_t to = smem_u32(sh.ring[0][0]) + my_row * kRowBytes + 16 * piece;
     auto ask = [&](int stage, int place) {
         if (stage < stages && k0 + stage * kStageK + 8 * piece < k1) {
@@ -366,14 +386,17 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_many_h_kernel(const __g
     extern __shared__ __align__(128) uint8_t smem[];
     Shared& sh = *reinterpret_cast<Shared*>(smem);
     const int ctas = p.cluster, cta = cluster_ctarank(), index = blockIdx.x / ctas, r0 = blockIdx.y * kRanks, ranks = p.n_parts * p.pad_rank;
-    const Workspace ws = views(p.h, p.items.n);
+    const Workspace ws = views(p.h, p.items);
     grid_dependency_wait();
     grid_launch_dependents();
     if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
     const Found item = find<kRankTiles, kManyRows>(p, index, sh);
     if (cta == 0 && blockIdx.y == 0) {
         if (static_cast<int>(threadIdx.x) < item.rows) ws.items[index].row[threadIdx.x] = sh.row[threadIdx.x];
-        if (threadIdx.x == 0) *reinterpret_cast<int4*>(&ws.items[index]) = make_int4(item.slot, item.rows, item.rank, 0);
+        if (threadIdx.x == 0) {
+            *reinterpret_cast<int4*>(&ws.items[index]) = make_int4(item.slot, item.rows, item.rank, 0);
+            if (index % p.items.per_window == 0) ws.counts[index / p.items.per_window] = p.base == p.y ? item.all - item.bare : item.all;
+        }
     }
     // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
     sum_h<kRankTiles, kManyRows>(p, item, r0, cta, ctas, sh);
@@ -500,10 +523,12 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_few_kernel(const __grid
     if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
     const Found item = find<kRankTiles, kFewRows>(p, index, sh);
     const int rows = item.rows, rank = item.rank, stride = ctas * kHWarps;
-    if (rank > 0 && lane == 0) {
-        // the first columns' share of B is on its way into L2 meanwhile
-        const Unit at = unit_of(p, cta * kHWarps + warp, 64);
-        if (at.n0 < at.end) prefetch_l2(p.B + (static_cast<long long>(item.slot) * p.N + at.n0) * p.max_rank, min(64, at.end - at.n0) * p.max_rank * 2);
+    if (rank > 0) {
+        // this warp's columns' share of B is on its way into L2 meanwhile
+        for (int unit = cta * kHWarps + warp + lane * stride; unit < units; unit += 32 * stride) {
+            const Unit at = unit_of(p, unit, 64);
+            prefetch_l2(p.B + (static_cast<long long>(item.slot) * p.N + at.n0) * p.max_rank, min(64, at.end - at.n0) * p.max_rank * 2);
+        }
     }
     const float scale = rank > 0 && p.scale ? p.scale[item.slot] : 1.0f;
     const int quads = rank > 0 ? rows * (kRanks / 4) : 0;
@@ -614,7 +639,7 @@ __global__ void __launch_bounds__(kManyThreads, kSteps16 == 1 ? 3 : 2) adapters_
     __shared__ int row_s[kManyRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
     const int pad_rank = p.pad_rank, quads = p.n_parts * pad_rank / 4, stride = b_stride(p.max_rank), stage_bytes = many_stage_bytes<T>(p.max_rank);
-    const Workspace ws = views(p.h, p.items.n);
+    const Workspace ws = views(p.h, p.items);
     const int index = blockIdx.x / units;
     const Unit at = unit_of(p, blockIdx.x - index * units, kCols * span);
     const Item& item = ws.items[index];
@@ -740,6 +765,321 @@ __global__ void __launch_bounds__(kManyThreads, kSteps16 == 1 ? 3 : 2) adapters_
     copies_wait<0>();
 }
 
+// Many rows, high ranks: the tensor core takes its operands from shared memory, and its accumulators are in tensor memory.  Tiles of an item's
+// rows and kRowBytes of each of them, in columns of one part; a CTA per SM has an equal share of all tiles, one
+// after another.  A tile of base comes into shared memory while the one before is done; the tensor core multiplies the item's h, which stays in
+// shared memory as 128 x 2 rank (hi, then lo against the same B), with the next tile's B into one of two accumulators in tensor memory
+// while the threads take this tile out of the other one, add base in its place, and store rows from there.
+// Operands lie in the tensor core's swizzled layout of 32, 64 or 128 bytes of K per row (a rank of 128 takes two such blocks): the pieces of a
+// row, which neighbouring threads copy, stay within 128 bytes.  (Without swizzle each goes to a line of shared memory of its own, and
+// the copies of one tile of B took 2500 cycles instead of 300.)  Rows of base: piece i of row r (16 bytes) at
+// i ^ (r & 7), so that eight threads with a row each meet no bank twice.
+constexpr int kHighThreads = 512, kHighWarps = kHighThreads / 32;
+struct HighShared { int k_bytes, blocks, h, base, b, total; };   // bytes of K per row, blocks of them; bytes of h, a tile of base, of B, and in all, with two of each tile
+__host__ __device__ inline HighShared high_shared(int pad_rank, int row_bytes, int cols) {
+    HighShared t;
+    t.k_bytes = pad_rank <= 16 ? 32 : pad_rank <= 32 ? 64 : 128;
+    t.blocks = pad_rank <= 64 ? 1 : 2;
+    t.h = 2 * t.blocks * kManyRows * t.k_bytes;
+    t.base = kManyRows * row_bytes;
+    t.b = t.blocks * cols * t.k_bytes;
+    t.total = 1024 + t.h + 2 * (t.base + t.b);   // (the first kilobyte: alignment)
+    return t;
+}
+// Where 16-byte piece c of row r of an operand with `rows` rows lies.
+__device__ __forceinline__ uint32_t operand_at(int r, int c, int rows, int k_bytes) {
+    if (k_bytes == 32) return r * 32 + 16 * (c ^ (r >> 2 & 1));
+    if (k_bytes == 64) return r * 64 + 16 * (c ^ (r >> 1 & 3));
+    return (c >> 3) * rows * 128 + r * 128 + 16 * ((c ^ r) & 7);
+}
+__device__ __forceinline__ uint64_t operand_desc(uint32_t at, int k_bytes) {
+    return make_smem_desc(at, 16, 8 * k_bytes, k_bytes == 32 ? kSwizzle32B : k_bytes == 64 ? kSwizzle64B : kSwizzle128B);
+}
+// The nth item of all windows that has something to do; -1 and the number of them in `all` if there are not so many.
+__device__ __forceinline__ int nth_item(const int* counts, const AdapterItems& t, int nth, int* shared, int* all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int sum = 0;
+    for (int w0 = 0; w0 < t.windows; w0 += kHighThreads) {
+        const int w = w0 + threadIdx.x, c = w < t.windows ? counts[w] : 0;
+        int before = c;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, before, d);
+            if (lane >= d) before += v;
+        }
+        if (lane == 31) shared[warp] = before;
+        if (threadIdx.x == 0) shared[kHighWarps] = -1;
+        __syncthreads();
+        int here = 0;
+        before += sum - c;
+        for (int i = 0; i < kHighWarps; ++i) {
+            if (i < warp) before += shared[i];
+            here += shared[i];
+        }
+        if (nth >= before && nth < before + c) shared[kHighWarps] = w * t.per_window + nth - before;
+        __syncthreads();
+        const int found = shared[kHighWarps];
+        __syncthreads();
+        if (found >= 0) return found;
+        sum += here;
+    }
+    *all = sum;
+    return -1;
+}
+
+template <class T, int kRowBytes>
+__global__ void __launch_bounds__(kHighThreads, 1) adapters_high_y_kernel(const __grid_constant__ AdapterParams p, int tiles_per_item) {
+    constexpr int kCols = kRowBytes / sizeof(T), kPieces = kRowBytes / 16, kPieceCols = 16 / sizeof(T), kTmemCols = 2 * kCols;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int row_s[kManyRows], search_s[kHighWarps + 1];
+    __shared__ __align__(8) uint64_t done[2];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_s;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int pad_rank = p.pad_rank, ranks = p.n_parts * pad_rank;
+    const HighShared lay = high_shared(pad_rank, kRowBytes, kCols);
+    uint8_t* base_tiles = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem) + 1023) & ~uintptr_t(1023));
+    uint8_t *h_tile = base_tiles + 2 * lay.base, *b_tiles = h_tile + lay.h;
+    const Workspace ws = views(p.h, p.items);
+    const bool in_place = p.base == p.y;
+    if (threadIdx.x == 0) {
+        mbar_init(smem_u32(&done[0]), 1);
+        mbar_init(smem_u32(&done[1]), 1);
+        abort_s = 0;
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    // This CTA's share of all tiles: [at_tile, stop_tile), counted item after item of those that have something to do.  (In one window, those
+    // are its first ones.)
+    int active = 0;
+    if (p.items.windows == 1) active = ws.counts[0];
+    else nth_item(ws.counts, p.items, 0x7fffffff, search_s, &active);
+    const long long all_tiles = static_cast<long long>(active) * tiles_per_item;
+    long long at_tile = all_tiles * blockIdx.x / gridDim.x;
+    const long long stop_tile = all_tiles * (blockIdx.x + 1) / gridDim.x;
+    unsigned count = 0;            // tiles that were multiplied: accumulator and phase
+    bool ok = true;
+#pragma unroll 1
+    while (at_tile < stop_tile) {
+        // ---- the tiles of one part of one item
+        const int nth = static_cast<int>(at_tile / tiles_per_item);
+        int in_item = static_cast<int>(at_tile - static_cast<long long>(nth) * tiles_per_item);
+        const int index = p.items.windows == 1 ? nth : nth_item(ws.counts, p.items, nth, search_s, &active);
+        const Item& item = ws.items[index];
+        int part = 0, n0 = 0, end = p.part_end[0];
+        while (true) {
+            const int n = (end - n0 + kCols - 1) / kCols;
+            if (in_item < n) break;
+            in_item -= n;
+            n0 = end;
+            end = p.part_end[++part];
+        }
+        n0 += in_item * kCols;
+        const int tiles = static_cast<int>(min(stop_tile - at_tile, static_cast<long long>((end - n0 + kCols - 1) / kCols)));
+        const int width = min(end - n0, kCols * tiles);
+        at_tile += tiles;
+        const int4 head = *reinterpret_cast<const int4*>(&item);
+        const int listed = threadIdx.x < kManyRows ? item.row[threadIdx.x] : 0;
+        const int slot = head.x, rows = head.y, rank = head.z;
+        if (rank == 0) {   // (of an adapter whose rank is 0: in place too)
+            if (!in_place) copy_rows<T>(p, item.row, rows, n0, n0 + width, threadIdx.x, kHighThreads);
+            continue;
+        }
+        if (static_cast<int>(threadIdx.x) < rows) {
+            row_s[threadIdx.x] = listed;
+        }
+        // B holds zeros behind the rank up to the end of the k step (h does too)
+        if (rank & 15)
+            for (int i = threadIdx.x; i < 2 * lay.b / 16; i += kHighThreads) reinterpret_cast<uint4*>(b_tiles)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+
+        const T* base = static_cast<const T*>(p.base) + n0;
+        T* y = static_cast<T*>(p.y) + n0;
+        const uint16_t* B = p.B + (static_cast<long long>(slot) * p.N + n0) * p.max_rank;
+        // What a thread copies of a tile, worked out once: a piece of every kRowsOn-th row of base ...
+        constexpr int kRowsOn = kHighThreads / kPieces, kMyRows = kManyRows / kRowsOn;
+        const int base_piece = threadIdx.x % kPieces, base_row = threadIdx.x / kPieces;
+        const T* base_from[kMyRows];   // null: no such row
+#pragma unroll
+        for (int i = 0; i < kMyRows; ++i) {
+            const int r = base_row + i * kRowsOn;
+            base_from[i] = r < rows ? base + row_s[r] * p.ldbase + base_piece * kPieceCols : nullptr;
+        }
+        const uint32_t base_to = smem_u32(base_tiles) + base_row * kRowBytes + 16 * (base_piece ^ (base_row & 7));
+        static_assert(kRowsOn % 8 == 0, "the swizzle of a thread's rows is the same");
+        // ... and of B pieces that are kHighThreads apart (a rank of 8, 16, 32, 64 or 128: the same one of every so many-th row)
+        const int b_whole = rank / 8, b_pieces = (rank + 7) / 8, b_row = threadIdx.x / b_pieces, b_piece = threadIdx.x - b_row * b_pieces;
+        const int b_rows_on = kHighThreads / b_pieces, b_pieces_on = kHighThreads - b_rows_on * b_pieces;
+        const bool b_regular = b_pieces_on == 0 && (rank & 7) == 0;
+        const uint16_t* b_from = B + static_cast<long long>(b_row) * p.max_rank + 8 * b_piece;
+        const uint32_t b_to = smem_u32(b_tiles) + operand_at(b_row, b_piece, kCols, lay.k_bytes);
+        const long long b_step = static_cast<long long>(b_rows_on) * p.max_rank, b_tile_step = static_cast<long long>(kCols) * p.max_rank;
+        auto ask_b = [&](int tile) {
+            if (tile < tiles) {
+                const int n = tile * kCols, here = min(kCols, width - n);
+                if (b_regular) {   // (b_rows_on is a multiple of 8: the swizzle of a thread's rows is the same)
+                    const uint16_t* from = b_from + tile * b_tile_step;
+                    uint32_t to = b_to + (tile & 1) * lay.b;
+                    for (int row = b_row; row < here; row += b_rows_on) {
+                        copy16(to, from);
+                        from += b_step;
+                        to += b_rows_on * (b_piece >= 8 ? 128 : lay.k_bytes);
+                    }
+                } else {
+                    for (int row = b_row, c = b_piece; row < here;) {
+                        const uint16_t* from = B + static_cast<long long>(n + row) * p.max_rank + 8 * c;
+                        const uint32_t off = (tile & 1) * lay.b + operand_at(row, c, kCols, lay.k_bytes);
+                        if (c < b_whole) {
+                            copy16(smem_u32(b_tiles) + off, from);
+                        } else {   // the piece that the rank ends in
+                            const uint4 v = *reinterpret_cast<const uint4*>(from);
+                            const uint2 first = masked(make_uint2(v.x, v.y), rank - 8 * c), second = masked(make_uint2(v.z, v.w), rank - 8 * c - 4);
+                            *reinterpret_cast<uint4*>(b_tiles + off) = make_uint4(first.x, first.y, second.x, second.y);
+                        }
+                        row += b_rows_on;
+                        c += b_pieces_on;
+                        if (c >= b_pieces) {
+                            c -= b_pieces;
+                            ++row;
+                        }
+                    }
+                }
+            }
+            copies_commit();
+        };
+        auto ask_base = [&](int tile) {
+            const int n = tile * kCols;
+            if (tile < tiles && n + (base_piece + 1) * kPieceCols <= width) {
+#pragma unroll
+                for (int i = 0; i < kMyRows; ++i)
+                    if (base_from[i]) copy16(base_to + (tile & 1) * lay.base + i * (kRowsOn * kRowBytes), base_from[i] + n);
+            }
+            copies_commit();
+        };
+        // h: hi, then lo (of four ranks each in the workspace, of eight here)
+        for (int m = warp; m < rows; m += kHighWarps) {
+            const uint2* from = reinterpret_cast<const uint2*>(ws.h + static_cast<long long>(row_s[m]) * (ranks / 4) + part * (pad_rank / 4));
+            for (int c = lane; c < pad_rank / 2; c += 32)
+                copy8(smem_u32(h_tile) + (c & 1) * (lay.h / 2) + operand_at(m, c >> 2, kManyRows, lay.k_bytes) + 8 * (c >> 1 & 1), from + c);
+        }
+        ask_b(0);
+        ask_base(0);
+        ask_b(1);
+        ask_base(1);
+
+        const uint64_t h_desc = operand_desc(smem_u32(h_tile), lay.k_bytes);
+        const int k_steps = (rank + 15) / 16;
+        auto multiply = [&](int tile) {   // one thread
+            const unsigned number = count + tile;
+            const uint64_t b_desc = operand_desc(smem_u32(b_tiles) + (tile & 1) * lay.b, lay.k_bytes);
+            for (int term = 0; term < 2; ++term)
+                for (int k = 0; k < k_steps; ++k) {
+                    // (16 of K: 32 bytes on; a block of 64 of K: the next one)
+                    const uint64_t h_at = h_desc + ((term * (lay.h / 2) + (k >> 2) * kManyRows * 128 + (k & 3) * 32) >> 4);
+                    const uint64_t b_at = b_desc + (((k >> 2) * kCols * 128 + (k & 3) * 32) >> 4);
+                    tc_mma_bf16(tmem + (number & 1) * kCols, h_at, b_at, make_idesc_bf16(kCols), term | k);
+                }
+            tc_commit(smem_u32(&done[number & 1]));
+        };
+        // Takes a tile out: a warp has 32 rows (the lanes of tensor memory that it can read) and a quarter of the columns, 64 bytes of each
+        // row at a time.
+        const int my_row = 32 * (warp & 3) + lane, quarter = warp >> 2;
+        constexpr int kRow = kPieces / 4, kAtOnce = 32 / kRow;   // lanes that store a row's quarter, rows at once
+        const int out_piece = quarter * kRow + lane % kRow, out_row = 32 * (warp & 3) + lane / kRow;
+        T* to[32 / kAtOnce];
+#pragma unroll
+        for (int i = 0; i < 32 / kAtOnce; ++i) {
+            const int r = out_row + kAtOnce * i;
+            to[i] = r < rows ? y + row_s[r] * p.ldy + out_piece * kPieceCols : nullptr;
+        }
+        auto take = [&](int tile) {
+            uint8_t* base_tile = base_tiles + (tile & 1) * lay.base;
+            const uint32_t sums = tmem + ((32u * (warp & 3)) << 16) + ((count + tile) & 1) * kCols + quarter * (kCols / 4);
+            uint8_t* mine = base_tile + my_row * kRowBytes;
+#pragma unroll
+            for (int part64 = 0; part64 < kPieces / 16; ++part64) {
+                constexpr int kHere = 4 * kPieceCols;   // columns in 64 bytes
+                uint32_t d[kHere];
+                if constexpr (kHere == 32) tmem_ld_32x32(sums + part64 * kHere, d);
+                else tmem_ld_32x16(sums + part64 * kHere, d);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int piece = quarter * (kPieces / 4) + 4 * part64 + i;
+                    uint4* at16 = reinterpret_cast<uint4*>(mine + 16 * (piece ^ (my_row & 7)));
+                    uint4 v = *at16;
+                    uint32_t* w = &v.x;
+                    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            w[j] = pack_bf16(bf16_lo(w[j]) + __uint_as_float(d[8 * i + 2 * j]), bf16_hi(w[j]) + __uint_as_float(d[8 * i + 2 * j + 1]));
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(__uint_as_float(w[j]) + __uint_as_float(d[4 * i + j]));
+                    }
+                    *at16 = v;
+                    // the last columns of a matrix whose width is no multiple of a piece
+                    const int n = tile * kCols + piece * kPieceCols, cols = width - n;
+                    if (cols > 0 && cols < kPieceCols && my_row < rows) {
+#pragma unroll
+                        for (int j = 0; j < kPieceCols; ++j)
+                            if (j < cols) y[row_s[my_row] * p.ldy + n + j] = static_cast<T>(static_cast<float>(base[row_s[my_row] * p.ldbase + n + j]) + __uint_as_float(d[i * kPieceCols + j]));
+                    }
+                }
+            }
+            __syncwarp();
+            const int n = tile * kCols;
+            if (n + (out_piece + 1) * kPieceCols <= width) {
+#pragma unroll
+                for (int i = 0; i < 32 / kAtOnce; ++i) {
+                    const int r = out_row + kAtOnce * i;
+                    if (to[i]) *reinterpret_cast<uint4*>(to[i] + n) = *reinterpret_cast<const uint4*>(base_tile + r * kRowBytes + 16 * (out_piece ^ (r & 7)));
+                }
+            }
+        };
+        copies_wait<3>();            // h and the first B
+        fence_proxy_async_smem();    // (what copies and threads wrote, before the tensor core reads it)
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+        if (threadIdx.x == 0) multiply(0);
+#pragma unroll 1
+        for (int tile = 0; tile < tiles; ++tile) {
+            copies_wait<1>();            // this tile's base and the next one's B
+            fence_proxy_async_smem();
+            tc_fence_before_sync();      // (the accumulator that is written next has been read)
+            __syncthreads();
+            tc_fence_after_sync();
+            if (tile + 1 < tiles && threadIdx.x == 0) multiply(tile + 1);
+            ok = ok && mbar_wait(smem_u32(&done[(count + tile) & 1]), (count + tile) >> 1 & 1, &abort_s);
+            tc_fence_after_sync();
+            if (ok) take(tile);
+            __syncthreads();             // (the tile's places are free)
+            ask_b(tile + 2);
+            ask_base(tile + 2);
+        }
+        copies_wait<0>();
+        count += tiles;
+        tc_fence_before_sync();
+        __syncthreads();
+        tc_fence_after_sync();
+    }
+    if (!ok && lane == 0) atomicExch(p.status, PRQ_ERR_TIMEOUT);
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tmem, kTmemCols);
+}
+
 template <class... Params, class... Args>
 cudaError_t launch_kernel(void (*kernel)(Params...), dim3 blocks, int threads, int cluster, size_t smem, cudaStream_t stream, const Args&... args) {
     cudaLaunchConfig_t cfg = {};
@@ -773,6 +1113,23 @@ cudaError_t with_tiles(int tiles, F&& f) {
     return tiles == 2 ? f(std::integral_constant<int, 2>()) : tiles == 4 ? f(std::integral_constant<int, 4>())
          : tiles == 6 ? f(std::integral_constant<int, 6>()) : f(std::integral_constant<int, 8>());
 }
+// Pieces of `width` columns of all parts.
+int pieces_of(const AdapterParams& p, int width) {
+    int n = 0;
+    for (int i = 0; i < p.n_parts; ++i) n += (p.part_end[i] - (i ? p.part_end[i - 1] : 0) + width - 1) / width;
+    return n;
+}
+template <class T, int kRowBytes>
+cudaError_t launch_high_y(const AdapterParams& p, int num_sms, cudaStream_t stream) {
+    static OncePerDevice once;
+    constexpr int kCols = kRowBytes / sizeof(T);
+    const auto kernel = adapters_high_y_kernel<T, kRowBytes>;
+    const cudaError_t e = allow_shared(once, kernel, high_shared(kRowBytes == 512 ? 64 : PRQ_ADAPTER_MAX_RANK, kRowBytes, kCols).total);
+    if (e != cudaSuccess) return e;
+    const int tiles = pieces_of(p, kCols);
+    const long long most = static_cast<long long>(tiles) * p.items.n;
+    return launch_kernel(kernel, dim3(static_cast<unsigned>(std::min<long long>(most, num_sms))), kHighThreads, 1, high_shared(p.pad_rank, kRowBytes, kCols).total, stream, p, tiles);
+}
 template <class T, int kSteps16>
 cudaError_t launch_many_y(const AdapterParams& p, int units, int span, cudaStream_t stream) {
     static OncePerDevice once;
@@ -780,12 +1137,6 @@ cudaError_t launch_many_y(const AdapterParams& p, int units, int span, cudaStrea
     const cudaError_t e = allow_shared(once, kernel, kManyStages * many_stage_bytes<T>(PRQ_ADAPTER_MAX_RANK));
     if (e != cudaSuccess) return e;
     return launch_kernel(kernel, dim3(units * p.items.n), kManyThreads, 1, kManyStages * many_stage_bytes<T>(p.max_rank), stream, p, units, span);
-}
-// Pieces of `width` columns of all parts.
-int pieces_of(const AdapterParams& p, int width) {
-    int n = 0;
-    for (int i = 0; i < p.n_parts; ++i) n += (p.part_end[i] - (i ? p.part_end[i - 1] : 0) + width - 1) / width;
-    return n;
 }
 template <class T>
 cudaError_t launch_few(const AdapterParams& p, cudaStream_t stream) {
@@ -813,13 +1164,18 @@ cudaError_t launch_many_h(const AdapterParams& p, cudaStream_t stream) {
     });
 }
 template <class T>
-cudaError_t launch_many_y(const AdapterParams& p, cudaStream_t stream) {
-    int span = 4;
-    if (const char* v = dev_knobs_enabled() ? std::getenv("PRQ_AD_PER") : nullptr) span = atoi(v);
+cudaError_t launch_many_y(const AdapterParams& p, int num_sms, cudaStream_t stream) {
+    // Tensor memory for ranks above 32 where a CTA has many tiles (gate / up of 4096 tokens, 16 tiles of 256 columns per SM: rank 64 125 us
+    // with mma.sync, 105 so; rank 32 84 and 98; q / k / v, five per SM: rank 64 68 either way, rank 32 42 and 54; 1024 tokens of gate / up,
+    // rank 64: 47 either way), and for ranks above 64, whose h mma.sync's registers do not hold.
+    const int items = (p.M + kManyRows - 1) / kManyRows;
+    if (p.pad_rank > 64) return launch_high_y<T, 256>(p, num_sms, stream);
+    if (p.pad_rank > 32 && static_cast<long long>(pieces_of(p, 512 / sizeof(T))) * items >= 8ll * num_sms) return launch_high_y<T, 512>(p, num_sms, stream);
+    // a CTA's tiles: one where there are few of them, up to four for less to set up
+    const int span = static_cast<int>(std::max<long long>(1, std::min<long long>(4, static_cast<long long>(pieces_of(p, kManyCols<T>)) * items / (6ll * num_sms))));
     const int units = pieces_of(p, kManyCols<T> * span), steps = p.pad_rank / 16;
     if (static_cast<long long>(units) * p.items.n > 0x7fffffffll) return cudaErrorInvalidValue;
-    return steps == 1 ? launch_many_y<T, 1>(p, units, span, stream) : steps == 2 ? launch_many_y<T, 2>(p, units, span, stream)
-         : steps <= 4 ? launch_many_y<T, 4>(p, units, span, stream) : launch_many_y<T, 8>(p, units, span, stream);
+    return steps == 1 ? launch_many_y<T, 1>(p, units, span, stream) : steps == 2 ? launch_many_y<T, 2>(p, units, span, stream) : launch_many_y<T, 4>(p, units, span, stream);
 }
 
 }  // namespace
@@ -828,7 +1184,7 @@ size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank) {
     const AdapterItems items = plan_items(M, n_slots);
     if (M <= kFewCall) return 0;
     const size_t ranks = n_parts * ((max_rank + 15) & ~15);
-    return items.n < 0 ? 0 : sizeof(Item) * items.n + 4 * ranks * static_cast<size_t>(M);
+    return items.n < 0 ? 0 : counts_bytes(items) + sizeof(Item) * items.n + 4 * ranks * static_cast<size_t>(M);
 }
 
 cudaError_t launch_adapters(const AdapterParams& in, bool bf16, int num_sms, cudaStream_t stream, int* launches) {
@@ -842,7 +1198,6 @@ cudaError_t launch_adapters(const AdapterParams& in, bool bf16, int num_sms, cud
     p.cluster = 1;
     for (int c = 2; c <= 8; ++c)
         if (static_cast<long long>(items) * passes * c <= num_sms / 18 * (18 / c) * c && p.K / 32 >= (few ? 8 : 4) * c) p.cluster = c;
-    if (const char* v = dev_knobs_enabled() ? std::getenv("PRQ_AD_CLUSTER") : nullptr) p.cluster = atoi(v);
     if (few) {
         const cudaError_t e = bf16 ? launch_few<__nv_bfloat16>(p, stream) : launch_few<float>(p, stream);
         *launches = e == cudaSuccess;
@@ -851,7 +1206,7 @@ cudaError_t launch_adapters(const AdapterParams& in, bool bf16, int num_sms, cud
     cudaError_t e = launch_many_h(p, stream);
     if (e != cudaSuccess) return e;
     ++*launches;
-    e = bf16 ? launch_many_y<__nv_bfloat16>(p, stream) : launch_many_y<float>(p, stream);
+    e = bf16 ? launch_many_y<__nv_bfloat16>(p, num_sms, stream) : launch_many_y<float>(p, num_sms, stream);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

@@ -244,6 +244,8 @@ struct AdapterParams {
     int M, K, N, n_slots, max_rank, n_parts;
     int cluster;                 // CTAs per cluster
     int pad_rank;                // max_rank in whole k steps of 16
+    int y_size;                  // bytes of an element of base and y
+    uint32_t base_ahead;         // bytes of each row of base that are asked for in L2 ahead
     AdapterItems items;
     int part_end[kMaxBatch];     // column behind each part
 };
