@@ -430,7 +430,8 @@ typedef struct prq_adapters {
 } prq_adapters;
 
 /* Scratch of one prq_linear_adapters call for M rows; it need not be cleared, and calls that may overlap need one each.
- * Returns 0 for invalid arguments, and where none is needed. */
+ * Returns 0 for invalid arguments, and where none is needed: up to 128 rows, and up to 16 rows per slot
+ * of the pool. */
 size_t prq_adapters_workspace_bytes(const prq_adapters *a, int M);
 
 /*   row_adapter  device, M int32: each row's slot.  A row whose entry is not in [0, n_slots) -- -1, say -- has no adapter.  Rows
@@ -440,13 +441,15 @@ size_t prq_adapters_workspace_bytes(const prq_adapters *a, int M);
  *                prq_fold_adapter.
  *   base         device, M x N, row stride ldbase, dtype y_dtype: the projection's output
  *   y            device out, M x N, row stride ldy, same type; may be `base` itself (with ldy == ldbase), must not overlap it
- *                otherwise.  Rows without an adapter get base's values (bit for bit; in place they are not touched), and
+ *                otherwise, nor x or the pool.  Rows without an adapter get base's values (bit for bit; in place they are not touched), and
  *                so do rows whose adapter has rank 0.
- *   workspace    device, prq_adapters_workspace_bytes(a, M) bytes, 16-byte aligned
+ *   workspace    device, prq_adapters_workspace_bytes(a, M) bytes, 16-byte aligned; may be NULL where that is 0
  * Both matrices 16-byte aligned, their strides multiples of 8 (bf16) or 4 (fp32) elements.  Buffers belong to the current device.
- * The kernels read row_adapter, ranks, scale, A and B when they run: a captured call follows what a program writes there.
+ * The kernels read row_adapter, ranks, scale, A and B when they run: a captured call follows what a program writes there before it is
+ * replayed.  None of them may change while the call runs.  One launch where no workspace is needed, two otherwise.  A wait in a kernel that
+ * ran out leaves PRQ_ERR_TIMEOUT in the device status (prq_last_device_status), and y incomplete.
  * A value that is not finite in x, or in an adapter, reaches the rows of that row's, of that adapter's requests only.
- * Errors: INVALID_ARG, ALIGNMENT, WORKSPACE, UNSUPPORTED_ARCH, CUDA.  M == 0 is a no-op. */
+ * Errors: INVALID_ARG (M of 2^23 rows and more among it), ALIGNMENT, WORKSPACE, UNSUPPORTED_ARCH, CUDA.  M == 0 is a no-op. */
 prq_status prq_linear_adapters(const prq_adapters *a, const int32_t *row_adapter, const void *x, int M, int ldx, const void *base,
                                int ldbase, void *y, int ldy, prq_dtype y_dtype, void *workspace, size_t workspace_bytes,
                                prq_stream_t stream);
@@ -508,7 +511,7 @@ typedef struct prq_heads {
     const void *x;             /* device */
     void *out;                 /* device */
     int64_t ldx, hsx, ldout, hsout;
-    int heads;                 /* 0: nothing (then x and out may be NULL) */
+    int heads;                 /* up to 65536; 0: nothing (then x and out may be NULL) */
     const float *weight;       /* device, head_dim factors of the norm, NULL: 1.  Not used by prq_rotate_heads */
 } prq_heads;
 

@@ -1,14 +1,14 @@
 // Low-rank adapters beside a projection: h = scale * x A^T with the adapter of each row, then y = base + h B^T.
 //
-// Two launches.  The first one finds, for each of its clusters, an item -- rows of one adapter, from anywhere in a window of 4096 rows -- and sums
-// h of its rows; the second one streams y past h.  Items are worked out on the device, so that a captured call follows its row table.
-// Sums are fp32; h goes into the second product as two bf16 terms (hi = bf16(h), lo = bf16(h - hi): 16 bits and more of its
-// significand), whose products with B the tensor cores sum in fp32.
+// An item is rows of one adapter, from anywhere in a window of 4096 rows.  Few rows: one launch, in which a cluster has an item, sums its h and adds
+// h B^T.  Many rows: two launches, the first one for h, the second one streams y past it.  Items are worked out on the device, so that a
+// captured call follows its row table.  Sums are fp32; h goes into the second product as two bf16 terms (hi = bf16(h), lo = bf16(h - hi):
+// 16 bits and more of its significand), whose products with B the tensor cores sum in fp32.
 //
-// Both products use mma.sync (16 x 8 x 16, bf16): with a rank of 16 to 64 they hold 16 to 128 flop per byte of y, too little for
-// its rate to become the bound.  Rows may stand in any order, and sums stay in the registers of the lane that stores them.  The order
-// of a reduction's elements is free, so the k index of every fragment is permuted such that a lane's share of a row is 16 (or 8)
-// contiguous bytes in both operands.
+// Up to rank 32 both products use mma.sync (16 x 8 x 16, bf16): they hold 16 to 64 flop per byte of y, too little for its rate to become the
+// bound.  Rows may stand in any order, and sums stay in the registers of the lane that stores them.  The order of a reduction's elements is
+// free, so the k index of every fragment is permuted such that a lane's share of a row is 16 (or 8) contiguous bytes in both operands.
+// With higher ranks the loads of fragments from shared memory become the bound of y, and many tiles go through tcgen05.mma.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -29,6 +29,7 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1
 __device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
     asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
+__device__ __forceinline__ void st_cluster(uint32_t addr, int v) { asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -65,9 +66,9 @@ struct Columns {
 };
 
 // ---------------------------------------------------------------- items
-// Up to 16 rows each where a call has few of them, so that there are many items; up to 128 otherwise, so that A and B are read seldom.
+// Up to 16 rows each, or up to 128, so that A and B are read seldom and h and y have whole tiles.
 constexpr int kFewRows = 16, kManyRows = 128;
-constexpr int kFewCall = 128;         // rows of a call up to which items are small
+constexpr int kFewCall = 128;         // rows of a call up to which items are small in any case
 constexpr int kWindow = 4096;         // rows that are put in the order of their adapters together
 constexpr int kSortedSlots = 511;     // pools of more adapters, and calls of up to 32 rows: 32 rows that follow one another are grouped
 
@@ -76,7 +77,11 @@ struct __align__(16) Item {
     int row[kManyRows];
 };
 
-// rows per window, items that a window may have, windows, items in all (-1: too many)
+// Small items where adapters may have fewer rows than such an item, too.  (q / k / v, rank 16, 1000 rows of a pool of 64: all of them in use
+// 23 us, with large items 80; four of them in use 23 and 18.  Pool of 500: 102 and 582, 23 and 18.  Pool of 4: 15 and 18, but rank 64 39 and 27.
+// Rank 64, 200 rows of a pool of 64: 46 and 130, four in use 38 and 14.)  And where rows are put in order 32 at a time.
+bool small_items(int M, int n_slots) { return M <= kFewCall || n_slots > kSortedSlots || M < kFewRows * n_slots; }
+// rows per window, items that a window may have, windows, items in all
 AdapterItems plan_items(int M, int n_slots) {
     AdapterItems t;
     if (n_slots > kSortedSlots) {
@@ -85,11 +90,10 @@ AdapterItems plan_items(int M, int n_slots) {
     } else {
         t.window = M < kWindow ? M : kWindow;
         const int kinds = n_slots + 1 < t.window ? n_slots + 1 : t.window;
-        t.per_window = t.window / (M <= kFewCall ? kFewRows : kManyRows) + kinds;   // whole ones, and a rest of each adapter
+        t.per_window = t.window / (small_items(M, n_slots) ? kFewRows : kManyRows) + kinds;   // whole ones, and a rest of each adapter
     }
     t.windows = static_cast<int>((M + static_cast<long long>(t.window) - 1) / t.window);
-    const long long n = static_cast<long long>(t.windows) * t.per_window;
-    t.n = n > 0x7fffffffll / 16 ? -1 : static_cast<int>(n);
+    t.n = t.windows * t.per_window;   // (under 2^23 rows: 31 bits hold that, and all grids)
     return t;
 }
 
@@ -104,10 +108,8 @@ struct FindShared {
 
 // The CTA's item: the index-th one of the window at m0.  Every thread keeps up to eight rows and their places among the rows of
 // their adapter (a warp's rows follow one another, so that the order is that of the rows and a prompt's stay together).
-template <int kItemRows>
+template <int kItemRows, int kSteps>
 __device__ __forceinline__ void find_item(const AdapterParams& p, int m0, int n, int index, FindShared& f) {
-    constexpr int kSteps = kItemRows == kFewRows ? 1 : kWindow / kHThreads;   // (what is executed once counts by its instructions' way here, too)
-    static_assert(kFewCall <= kHThreads, "few rows: one step");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kinds = p.n_slots + 1;
     const int steps = (n + kHThreads - 1) / kHThreads, begin = warp * steps * 32;
     int slot[kSteps], place[kSteps];
@@ -187,10 +189,10 @@ __device__ __forceinline__ void find_item(const AdapterParams& p, int m0, int n,
     __syncthreads();
 }
 
-// The same within 32 rows that follow one another, for any number of adapters, by one warp: items in the order of their first rows, those without an
-// adapter last.
-template <int kItemRows>
+// The same for small items within 32 rows that follow one another, for any number of adapters, by one warp: items in the order of their
+// first rows, those without an adapter last.
 __device__ __forceinline__ void find_item_of_32(const AdapterParams& p, int m0, int n, int index, FindShared& f) {
+    constexpr int kItemRows = kFewRows;
     if (threadIdx.x < 32) {
         const int lane = threadIdx.x;
         int slot = lane < n ? p.row_adapter[m0 + lane] : -2;
@@ -258,13 +260,13 @@ struct HShared {
     int row[kItemRows];
 };
 struct Found { int slot, rows, rank, all, bare; };
-// The cluster's item, its rows in sh.row.
+// The nth item of a window, its rows in sh.row.
 template <int kRankTiles, int kItemRows>
-__device__ __forceinline__ Found find(const AdapterParams& p, int index, HShared<kRankTiles, kItemRows>& sh) {
-    const int window = p.items.windows == 1 ? 0 : index / p.items.per_window, m0 = window * p.items.window, n = min(p.items.window, p.M - m0);
-    const int nth = index - window * p.items.per_window;
-    if (p.n_slots > kSortedSlots || p.M <= 32) find_item_of_32<kItemRows>(p, m0, n, nth, sh.find);
-    else find_item<kItemRows>(p, m0, n, nth, sh.find);
+__device__ __forceinline__ Found find(const AdapterParams& p, int window, int nth, HShared<kRankTiles, kItemRows>& sh) {
+    const int m0 = window * p.items.window, n = min(p.items.window, p.M - m0);
+    if (kItemRows == kFewRows && (p.n_slots > kSortedSlots || p.M <= 32)) find_item_of_32(p, m0, n, nth, sh.find);
+    else if (kItemRows == kFewRows && n <= kHThreads) find_item<kItemRows, 1>(p, m0, n, nth, sh.find);   // (what is executed once counts by its instructions' way here, too)
+    else find_item<kItemRows, kWindow / kHThreads>(p, m0, n, nth, sh.find);
     Found f{sh.find.slot, sh.find.rows, 0, sh.find.all, sh.find.bare};
     if (static_cast<int>(threadIdx.x) < f.rows) sh.row[threadIdx.x] = sh.find.row[threadIdx.x];
     if (f.rows > 0 && f.slot >= 0 && f.slot < p.n_slots) f.rank = p.ranks ? min(max(p.ranks[f.slot], 0), p.max_rank) : p.max_rank;
@@ -369,8 +371,9 @@ __device__ __forceinline__ uint4 two_terms(float4 sum, float scale, int r, int r
     uint4 h;
     h.x = pack_bf16(v[0], v[1]);
     h.y = pack_bf16(v[2], v[3]);
-    h.z = pack_bf16(v[0] - bf16_lo(h.x), v[1] - bf16_hi(h.x));
-    h.w = pack_bf16(v[2] - bf16_lo(h.y), v[3] - bf16_hi(h.y));
+    const auto rest = [](float v, float hi) { return fabsf(hi) <= 3.4e38f ? v - hi : 0.0f; };   // (an infinite sum stays one)
+    h.z = pack_bf16(rest(v[0], bf16_lo(h.x)), rest(v[1], bf16_hi(h.x)));
+    h.w = pack_bf16(rest(v[2], bf16_lo(h.y)), rest(v[3], bf16_hi(h.y)));
     return h;
 }
 
@@ -378,53 +381,64 @@ __device__ __forceinline__ uint4 two_terms(float4 sum, float scale, int r, int r
 template <int kRankTiles>
 struct ManyHShared : HShared<kRankTiles, kManyRows> {
     float4 got[kManyRows * 8 * kRankTiles / 4 + 8];   // sums of the cluster's CTAs for this CTA's share of them, one CTA behind the other
+    int todo;                                         // items of the window that have something to do, as the cluster's first CTA found them
 };
-template <int kRankTiles>
+template <int kRankTiles, bool kOnce>
 __global__ void __launch_bounds__(kHThreads, 1) adapters_many_h_kernel(const __grid_constant__ AdapterParams p) {
     using Shared = ManyHShared<kRankTiles>;
     constexpr int kRanks = Shared::kRanks;
     extern __shared__ __align__(128) uint8_t smem[];
     Shared& sh = *reinterpret_cast<Shared*>(smem);
-    const int ctas = p.cluster, cta = cluster_ctarank(), index = blockIdx.x / ctas, r0 = blockIdx.y * kRanks, ranks = p.n_parts * p.pad_rank;
+    const int ctas = p.cluster, cta = cluster_ctarank(), r0 = blockIdx.y * kRanks, ranks = p.n_parts * p.pad_rank;
+    const int window = blockIdx.x / ctas / p.h_clusters, begin = blockIdx.x / ctas - window * p.h_clusters;
     const Workspace ws = views(p.h, p.items);
     grid_dependency_wait();
     grid_launch_dependents();
-    if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
-    const Found item = find<kRankTiles, kManyRows>(p, index, sh);
-    if (cta == 0 && blockIdx.y == 0) {
-        if (static_cast<int>(threadIdx.x) < item.rows) ws.items[index].row[threadIdx.x] = sh.row[threadIdx.x];
-        if (threadIdx.x == 0) {
-            *reinterpret_cast<int4*>(&ws.items[index]) = make_int4(item.slot, item.rows, item.rank, 0);
-            if (index % p.items.per_window == 0) ws.counts[index / p.items.per_window] = p.base == p.y ? item.all - item.bare : item.all;
+    int nth = begin;
+    while (true) {
+        if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
+        const Found item = find<kRankTiles, kManyRows>(p, window, nth, sh);
+        const int todo = p.base == p.y ? item.all - item.bare : item.all;
+        if (cta == 0 && blockIdx.y == 0) {
+            Item& to = ws.items[window * p.items.per_window + nth];
+            if (static_cast<int>(threadIdx.x) < item.rows) to.row[threadIdx.x] = sh.row[threadIdx.x];
+            if (threadIdx.x == 0) {
+                *reinterpret_cast<int4*>(&to) = make_int4(item.slot, item.rows, item.rank, 0);
+                if (nth == 0) ws.counts[window] = todo;
+            }
         }
-    }
-    // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
-    sum_h<kRankTiles, kManyRows>(p, item, r0, cta, ctas, sh);
-    // the cluster's sums: a share of them in each CTA
-    const int quads = (item.rank > 0 ? item.rows : 0) * (kRanks / 4), share = (quads + ctas - 1) / ctas;
-    const float to_share = share > 0 ? 1.0f / share : 0.0f;
-    if (ctas > 1) cluster_wait();
-    for (int i = threadIdx.x; i < quads; i += kHThreads) {
-        const int c = __float2int_rd((i + 0.5f) * to_share);   // i / share (i + 0.5 is 2^-13 of itself and more away from a border)
-        st_cluster(cluster_map(smem_u32(&sh.got[cta * share + i - c * share]), c), cta_sum(sh, i / (kRanks / 4), i % (kRanks / 4) * 4));
-    }
-    const float scale = item.rank > 0 && p.scale ? p.scale[item.slot] : 1.0f;
-    if (ctas > 1) {
-        cluster_arrive();
-        cluster_wait();
-    } else {
-        __syncthreads();
-    }
-    const int i0 = min(quads, share * cta), mine = min(quads, i0 + share) - i0;
-    for (int i = threadIdx.x; i < mine; i += kHThreads) {
-        const int m = (i0 + i) / (kRanks / 4), f = r0 + (i0 + i) % (kRanks / 4) * 4;
-        if (f >= ranks) continue;
-        float4 sum = sh.got[i];
-        for (int k = 1; k < ctas; ++k) {
-            const float4 u = sh.got[k * share + i];
-            sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+        // (a cluster without work meets all the same: the number of meetings does not depend on what each CTA read, but on what its first one did)
+        sum_h<kRankTiles, kManyRows>(p, item, r0, cta, ctas, sh);
+        // the cluster's sums: a share of them in each CTA
+        const int quads = (item.rank > 0 ? item.rows : 0) * (kRanks / 4), share = (quads + ctas - 1) / ctas;
+        const float to_share = share > 0 ? 1.0f / share : 0.0f;
+        if (ctas > 1) cluster_wait();
+        for (int i = threadIdx.x; i < quads; i += kHThreads) {
+            const int c = __float2int_rd((i + 0.5f) * to_share);   // i / share (i + 0.5 is 2^-13 of itself and more away from a border)
+            st_cluster(cluster_map(smem_u32(&sh.got[cta * share + i - c * share]), c), cta_sum(sh, i / (kRanks / 4), i % (kRanks / 4) * 4));
         }
-        ws.h[static_cast<long long>(sh.row[m]) * (ranks / 4) + f / 4] = two_terms(sum, scale, f - part_of(f, p.pad_rank) * p.pad_rank, item.rank);
+        if (!kOnce && cta == 0 && static_cast<int>(threadIdx.x) < ctas) st_cluster(cluster_map(smem_u32(&sh.todo), threadIdx.x), todo);
+        const float scale = item.rank > 0 && p.scale ? p.scale[item.slot] : 1.0f;
+        if (ctas > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        const int i0 = min(quads, share * cta), mine = min(quads, i0 + share) - i0;
+        for (int i = threadIdx.x; i < mine; i += kHThreads) {
+            const int m = (i0 + i) / (kRanks / 4), f = r0 + (i0 + i) % (kRanks / 4) * 4;
+            if (f >= ranks) continue;
+            float4 sum = sh.got[i];
+            for (int k = 1; k < ctas; ++k) {
+                const float4 u = sh.got[k * share + i];
+                sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+            }
+            ws.h[static_cast<long long>(sh.row[m]) * (ranks / 4) + f / 4] = two_terms(sum, scale, f - part_of(f, p.pad_rank) * p.pad_rank, item.rank);
+        }
+        nth += p.h_clusters;
+        if (kOnce || nth >= sh.todo) break;
+        __syncthreads();   // (rows and sums have been read)
     }
 }
 
@@ -471,21 +485,18 @@ __device__ __forceinline__ void add_last(const float (&acc)[4][4], int e, int co
     for (int n = 0; n < 8; ++n)
         if (n < cols) to[n] = static_cast<T>(static_cast<float>(from[n]) + acc[n / 2][e + (n & 1)]);
 }
-// Part and columns of the unit-th `width` columns of y.
+// Part and columns of the unit-th `width` columns of y (p.unit_end: units up to the end of each part).
 struct Unit { int part, n0, end; };
 __device__ __forceinline__ Unit unit_of(const AdapterParams& p, int unit, int width) {
-    int part = 0, from = 0;
+    int part = 0, first = 0, from = 0;
 #pragma unroll
-    for (int i = 0; i < kMaxBatch - 1; ++i) {
-        if (part != i || i >= p.n_parts - 1) continue;
-        const int n = (p.part_end[i] - from + width - 1) / width;
-        if (unit >= n) {
-            unit -= n;
+    for (int i = 0; i < kMaxBatch - 1; ++i)
+        if (unit >= p.unit_end[i]) {   // (of parts that do not exist: all units)
+            part = i + 1;
+            first = p.unit_end[i];
             from = p.part_end[i];
-            ++part;
         }
-    }
-    return Unit{part, from + width * unit, p.part_end[part]};
+    return Unit{part, from + width * (unit - first), p.part_end[part]};
 }
 // Rows without an adapter, where y is not base: copied bit for bit.
 template <class T>
@@ -509,114 +520,123 @@ template <int kRankTiles>
 struct FewShared : HShared<kRankTiles, kFewRows> {
     uint4 h[kFewRows * PRQ_MULTI_MAX * PRQ_ADAPTER_MAX_RANK / 4];   // [rank / 4][row]
     float4 got[8][kFewRows * 8 * kRankTiles / 4];                    // from each CTA of the cluster
+    int todo;                                                        // as above
 };
-template <class T, int kRankTiles>
+template <class T, int kRankTiles, bool kOnce>
 __global__ void __launch_bounds__(kHThreads, 1) adapters_few_kernel(const __grid_constant__ AdapterParams p, int passes, int units) {
     using Shared = FewShared<kRankTiles>;
     constexpr int kRanks = Shared::kRanks;
     extern __shared__ __align__(128) uint8_t smem[];
     Shared& sh = *reinterpret_cast<Shared*>(smem);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-    const int ctas = p.cluster, cta = cluster_ctarank(), index = blockIdx.x / ctas, pad_rank = p.pad_rank, ranks = p.n_parts * pad_rank;
+    const int ctas = p.cluster, cta = cluster_ctarank(), pad_rank = p.pad_rank, ranks = p.n_parts * pad_rank;
+    const int window = blockIdx.x / ctas / p.h_clusters;
+    int nth = blockIdx.x / ctas - window * p.h_clusters;
     grid_dependency_wait();
     grid_launch_dependents();
-    if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
-    const Found item = find<kRankTiles, kFewRows>(p, index, sh);
-    const int rows = item.rows, rank = item.rank, stride = ctas * kHWarps;
-    if (rank > 0) {
-        // this warp's columns' share of B is on its way into L2 meanwhile
-        for (int unit = cta * kHWarps + warp + lane * stride; unit < units; unit += 32 * stride) {
-            const Unit at = unit_of(p, unit, 64);
-            prefetch_l2(p.B + (static_cast<long long>(item.slot) * p.N + at.n0) * p.max_rank, min(64, at.end - at.n0) * p.max_rank * 2);
+    while (true) {
+        if (ctas > 1) cluster_arrive();   // (the others' shared memory may be written to once all have come by here)
+        const Found item = find<kRankTiles, kFewRows>(p, window, nth, sh);
+        const int rows = item.rows, rank = item.rank, stride = ctas * kHWarps;
+        if (rank > 0) {
+            // this warp's columns' share of B is on its way into L2 meanwhile
+            for (int unit = cta * kHWarps + warp + lane * stride; unit < units; unit += 32 * stride) {
+                const Unit at = unit_of(p, unit, 64);
+                prefetch_l2(p.B + (static_cast<long long>(item.slot) * p.N + at.n0) * p.max_rank, min(64, at.end - at.n0) * p.max_rank * 2);
+            }
         }
-    }
-    const float scale = rank > 0 && p.scale ? p.scale[item.slot] : 1.0f;
-    const int quads = rank > 0 ? rows * (kRanks / 4) : 0;
-    // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
-    for (int pass = 0; pass < passes; ++pass) {
-        sum_h<kRankTiles, kFewRows>(p, item, pass * kRanks, cta, ctas, sh);
-        if (ctas > 1) cluster_wait();
-        for (int i = threadIdx.x; i < quads; i += kHThreads) {
-            const float4 sum = cta_sum(sh, i / (kRanks / 4), i % (kRanks / 4) * 4);
-            for (int c = 0; c < ctas; ++c) st_cluster(cluster_map(smem_u32(&sh.got[cta][i]), c), sum);
-        }
-        if (ctas > 1) {
-            cluster_arrive();
-            cluster_wait();
-        } else {
+        const float scale = rank > 0 && p.scale ? p.scale[item.slot] : 1.0f;
+        const int quads = rank > 0 ? rows * (kRanks / 4) : 0;
+        // (a cluster without work meets all the same, so that the number of meetings does not depend on what each CTA read)
+        for (int pass = 0; pass < passes; ++pass) {
+            sum_h<kRankTiles, kFewRows>(p, item, pass * kRanks, cta, ctas, sh);
+            if (ctas > 1) cluster_wait();
+            for (int i = threadIdx.x; i < quads; i += kHThreads) {
+                const float4 sum = cta_sum(sh, i / (kRanks / 4), i % (kRanks / 4) * 4);
+                for (int c = 0; c < ctas; ++c) st_cluster(cluster_map(smem_u32(&sh.got[cta][i]), c), sum);
+            }
+            if (!kOnce && cta == 0 && static_cast<int>(threadIdx.x) < ctas) st_cluster(cluster_map(smem_u32(&sh.todo), threadIdx.x), p.base == p.y ? item.all - item.bare : item.all);
+            if (ctas > 1) {
+                cluster_arrive();
+                cluster_wait();
+            } else {
+                __syncthreads();
+            }
+            for (int i = threadIdx.x; i < quads; i += kHThreads) {
+                const int m = i / (kRanks / 4), f = pass * kRanks + i % (kRanks / 4) * 4;
+                if (f >= ranks) continue;
+                float4 sum = sh.got[0][i];
+                for (int c = 1; c < ctas; ++c) {
+                    const float4 u = sh.got[c][i];
+                    sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
+                }
+                sh.h[f / 4 * kFewRows + m] = two_terms(sum, scale, f - part_of(f, pad_rank) * pad_rank, rank);
+            }
             __syncthreads();
+            if (ctas > 1 && pass + 1 < passes) cluster_arrive();   // (what was got has been read)
         }
-        for (int i = threadIdx.x; i < quads; i += kHThreads) {
-            const int m = i / (kRanks / 4), f = pass * kRanks + i % (kRanks / 4) * 4;
-            if (f >= ranks) continue;
-            float4 sum = sh.got[0][i];
-            for (int c = 1; c < ctas; ++c) {
-                const float4 u = sh.got[c][i];
-                sum.x += u.x; sum.y += u.y; sum.z += u.z; sum.w += u.w;
-            }
-            sh.h[f / 4 * kFewRows + m] = two_terms(sum, scale, f - part_of(f, pad_rank) * pad_rank, rank);
-        }
-        __syncthreads();
-        if (ctas > 1 && pass + 1 < passes) cluster_arrive();   // (what was got has been read)
-    }
 
-    const bool mine[2] = {g < rows, 8 + g < rows};
-    // (lanes whose row does not exist repeat the item's first one up to the store)
-    const long long row[2] = {mine[0] ? sh.row[g] : 0, mine[1] ? sh.row[8 + g] : 0};
+        const bool mine[2] = {g < rows, 8 + g < rows};
+        // (lanes whose row does not exist repeat the item's first one up to the store)
+        const long long row[2] = {mine[0] ? sh.row[g] : 0, mine[1] ? sh.row[8 + g] : 0};
 #pragma unroll 1
-    for (int unit = cta * kHWarps + warp; unit < units && rows > 0; unit += stride) {
-        const Unit at = unit_of(p, unit, 64);
-        if (rank == 0) {
-            if (p.base != p.y) copy_rows<T>(p, sh.row, rows, at.n0, min(at.end, at.n0 + 64), lane, 32);
-            continue;
-        }
-        Columns<T> v[2][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int col = at.n0 + 32 * j + 8 * q;
-                v[i][j] = Columns<T>{};
-                if (mine[i] && col + 8 <= at.end) v[i][j].load(static_cast<const T*>(p.base) + row[i] * p.ldbase + col);
+        for (int unit = cta * kHWarps + warp; unit < units && rows > 0; unit += stride) {
+            const Unit at = unit_of(p, unit, 64);
+            if (rank == 0) {
+                if (p.base != p.y) copy_rows<T>(p, sh.row, rows, at.n0, min(at.end, at.n0 + 64), lane, 32);
+                continue;
             }
-        float acc[2][4][4];
-        const uint16_t* B = p.B + (static_cast<long long>(item.slot) * p.N + at.n0 + 8 * (g >> 1) + (g & 1)) * p.max_rank + 4 * q;
-        const uint4* H = sh.h + (at.part * (pad_rank / 4) + q) * kFewRows + g;
-        const int n_left = at.end - at.n0 - 8 * (g >> 1) - (g & 1);   // columns of this lane's row of B up to the end
+            Columns<T> v[2][2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int col = at.n0 + 32 * j + 8 * q;
+                    v[i][j] = Columns<T>{};
+                    if (mine[i] && col + 8 <= at.end) v[i][j].load(static_cast<const T*>(p.base) + row[i] * p.ldbase + col);
+                }
+            float acc[2][4][4];
+            const uint16_t* B = p.B + (static_cast<long long>(item.slot) * p.N + at.n0 + 8 * (g >> 1) + (g & 1)) * p.max_rank + 4 * q;
+            const uint4* H = sh.h + (at.part * (pad_rank / 4) + q) * kFewRows + g;
+            const int n_left = at.end - at.n0 - 8 * (g >> 1) - (g & 1);   // columns of this lane's row of B up to the end
 #pragma unroll 1
-        for (int k = 0; k < rank; k += 16) {
-            const int left = rank - k - 4 * q;
-            uint2 b[8];
+            for (int k = 0; k < rank; k += 16) {
+                const int left = rank - k - 4 * q;
+                uint2 b[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int n = 32 * (j / 4) + 2 * (j % 4);
-                b[j] = make_uint2(0, 0);
-                if (n < n_left && left > 0) b[j] = *reinterpret_cast<const uint2*>(B + static_cast<long long>(n) * p.max_rank + k);
+                for (int j = 0; j < 8; ++j) {
+                    const int n = 32 * (j / 4) + 2 * (j % 4);
+                    b[j] = make_uint2(0, 0);
+                    if (n < n_left && left > 0) b[j] = *reinterpret_cast<const uint2*>(B + static_cast<long long>(n) * p.max_rank + k);
+                }
+                const uint4 ha = H[k / 4 * kFewRows], hb = H[k / 4 * kFewRows + 8];   // (of a row that does not exist: reaches no sum that is stored)
+                if (k == 0) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) begin_sum<T>(acc[j], v[i][j], 2 * i);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    if (left < 4) b[j] = masked(b[j], left);
+                    mma_bf16(acc[j / 4][j % 4], ha.x, hb.x, ha.y, hb.y, b[j].x, b[j].y);
+                    mma_bf16(acc[j / 4][j % 4], ha.z, hb.z, ha.w, hb.w, b[j].x, b[j].y);
+                }
             }
-            const uint4 ha = H[k / 4 * kFewRows], hb = H[k / 4 * kFewRows + 8];   // (of a row that does not exist: reaches no sum that is stored)
-            if (k == 0) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) begin_sum<T>(acc[j], v[i][j], 2 * i);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (left < 4) b[j] = masked(b[j], left);
-                mma_bf16(acc[j / 4][j % 4], ha.x, hb.x, ha.y, hb.y, b[j].x, b[j].y);
-                mma_bf16(acc[j / 4][j % 4], ha.z, hb.z, ha.w, hb.w, b[j].x, b[j].y);
-            }
+                for (int j = 0; j < 2; ++j) {
+                    const int col = at.n0 + 32 * j + 8 * q, cols = at.end - col;
+                    if (!mine[i] || cols <= 0) continue;
+                    T* to = static_cast<T*>(p.y) + row[i] * p.ldy + col;
+                    if (cols >= 8) end_sum<T>(acc[j], v[i][j], 2 * i).store(to);
+                    else add_last<T>(acc[j], 2 * i, cols, static_cast<const T*>(p.base) + row[i] * p.ldbase + col, to);
+                }
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int col = at.n0 + 32 * j + 8 * q, cols = at.end - col;
-                if (!mine[i] || cols <= 0) continue;
-                T* to = static_cast<T*>(p.y) + row[i] * p.ldy + col;
-                if (cols >= 8) end_sum<T>(acc[j], v[i][j], 2 * i).store(to);
-                else add_last<T>(acc[j], 2 * i, cols, static_cast<const T*>(p.base) + row[i] * p.ldbase + col, to);
-            }
+        nth += p.h_clusters;
+        if (kOnce || nth >= sh.todo) break;
+        __syncthreads();   // (rows and sums have been read)
     }
 }
 
@@ -640,129 +660,133 @@ __global__ void __launch_bounds__(kManyThreads, kSteps16 == 1 ? 3 : 2) adapters_
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
     const int pad_rank = p.pad_rank, quads = p.n_parts * pad_rank / 4, stride = b_stride(p.max_rank), stage_bytes = many_stage_bytes<T>(p.max_rank);
     const Workspace ws = views(p.h, p.items);
-    const int index = blockIdx.x / units;
-    const Unit at = unit_of(p, blockIdx.x - index * units, kCols * span);
-    const Item& item = ws.items[index];
+    const int turn = blockIdx.x / units, window = turn / p.y_items;
+    const Unit at = unit_of(p, blockIdx.x - turn * units, kCols * span);
     const int stop = min(at.end, at.n0 + kCols * span), tiles = (stop - at.n0 + kCols - 1) / kCols;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int4 head = *reinterpret_cast<const int4*>(&item);
-    const int listed = threadIdx.x < kManyRows ? item.row[threadIdx.x] : 0;
-    const int slot = head.x, rows = head.y, rank = head.z;
-    if (rows == 0) return;
-    if (rank == 0) {
-        if (p.base != p.y) copy_rows<T>(p, item.row, rows, at.n0, stop, threadIdx.x, kManyThreads);
-        return;
-    }
-    if (static_cast<int>(threadIdx.x) < rows) {
-        row_s[threadIdx.x] = listed;
-        base_s[threadIdx.x] = static_cast<const T*>(p.base) + listed * p.ldbase + at.n0;
-    }
-    __syncthreads();
+    for (int nth = turn - window * p.y_items, todo = 0x7fffffff; nth < todo; nth += p.y_items) {
+        const Item& item = ws.items[window * p.items.per_window + nth];
+        todo = ws.counts[window];
+        const int4 head = *reinterpret_cast<const int4*>(&item);
+        const int listed = threadIdx.x < kManyRows ? item.row[threadIdx.x] : 0;
+        const int slot = head.x, rows = head.y, rank = head.z;
+        if (nth >= todo) return;
+        if (rank == 0) {
+            if (p.base != p.y) copy_rows<T>(p, item.row, rows, at.n0, stop, threadIdx.x, kManyThreads);
+            continue;
+        }
+        if (static_cast<int>(threadIdx.x) < rows) {
+            row_s[threadIdx.x] = listed;
+            base_s[threadIdx.x] = static_cast<const T*>(p.base) + listed * p.ldbase + at.n0;
+        }
+        __syncthreads();
 
-    // a thread copies one piece of every kRowStep-th row of base, and of one row of B one in kBThreads
-    constexpr int kRowStep = kManyThreads / 8, kBThreads = kManyThreads / kCols;
-    const int piece = threadIdx.x & 7, b_row = threadIdx.x / kBThreads, in = b_row & 31;
-    const T* base_from[kManyRows / kRowStep];
+        // a thread copies one piece of every kRowStep-th row of base, and of one row of B one in kBThreads
+        constexpr int kRowStep = kManyThreads / 8, kBThreads = kManyThreads / kCols;
+        const int piece = threadIdx.x & 7, b_row = threadIdx.x / kBThreads, in = b_row & 31;
+        const T* base_from[kManyRows / kRowStep];
 #pragma unroll
-    for (int i = 0; i < kManyRows / kRowStep; ++i) {
-        const int r = (threadIdx.x >> 3) + i * kRowStep;
-        base_from[i] = r < rows ? base_s[r] + piece * kPieceCols : nullptr;
-    }
-    const uint32_t base_to = smem_u32(smem) + (threadIdx.x >> 3) * 128 + 16 * (piece ^ ((threadIdx.x >> 3 & 1) << 2));   // (kRowStep is even)
-    const uint16_t* b_from = p.B + (static_cast<long long>(slot) * p.N + at.n0 + b_row) * p.max_rank + 8 * (threadIdx.x % kBThreads);
-    const uint32_t b_to = smem_u32(smem) + kManyRows * 128 + ((b_row & ~31) + 8 * ((in & 7) >> 1) + 2 * (in >> 3) + (in & 1)) * stride + 16 * (threadIdx.x % kBThreads);
-    const int b_pieces = p.max_rank / 8 - threadIdx.x % kBThreads, width = stop - at.n0;
-    auto ask = [&](int tile, int place) {
-        const int n = tile * kCols;
-        if (n + (piece + 1) * kPieceCols <= width) {
-#pragma unroll
-            for (int i = 0; i < kManyRows / kRowStep; ++i)
-                if (base_from[i]) copy16(base_to + place * stage_bytes + i * (kRowStep * 128), base_from[i] + n);
+        for (int i = 0; i < kManyRows / kRowStep; ++i) {
+            const int r = (threadIdx.x >> 3) + i * kRowStep;
+            base_from[i] = r < rows ? base_s[r] + piece * kPieceCols : nullptr;
         }
-        if (n + b_row < width) {
-            const uint16_t* b = b_from + static_cast<long long>(n) * p.max_rank;
-            for (int i = 0; i < b_pieces; i += kBThreads) copy16(b_to + place * stage_bytes + 16 * i, b + 8 * i);
-        }
-        copies_commit();
-    };
+        const uint32_t base_to = smem_u32(smem) + (threadIdx.x >> 3) * 128 + 16 * (piece ^ ((threadIdx.x >> 3 & 1) << 2));   // (kRowStep is even)
+        const uint16_t* b_from = p.B + (static_cast<long long>(slot) * p.N + at.n0 + b_row) * p.max_rank + 8 * (threadIdx.x % kBThreads);
+        const uint32_t b_to = smem_u32(smem) + kManyRows * 128 + ((b_row & ~31) + 8 * ((in & 7) >> 1) + 2 * (in >> 3) + (in & 1)) * stride + 16 * (threadIdx.x % kBThreads);
+        const int b_pieces = p.max_rank / 8 - threadIdx.x % kBThreads, width = stop - at.n0;
+        auto ask = [&](int tile, int place) {
+            const int n = tile * kCols;
+            if (n + (piece + 1) * kPieceCols <= width) {
 #pragma unroll
-    for (int i = 0; i < kManyStages - 1; ++i) ask(i, i);
+                for (int i = 0; i < kManyRows / kRowStep; ++i)
+                    if (base_from[i]) copy16(base_to + place * stage_bytes + i * (kRowStep * 128), base_from[i] + n);
+            }
+            if (n + b_row < width) {
+                const uint16_t* b = b_from + static_cast<long long>(n) * p.max_rank;
+                for (int i = 0; i < b_pieces; i += kBThreads) copy16(b_to + place * stage_bytes + 16 * i, b + 8 * i);
+            }
+            copies_commit();
+        };
+#pragma unroll
+        for (int i = 0; i < kManyStages - 1; ++i) ask(i, i);
 
-    // h of rows g and 8 + g of the warp's 16 (of a row that exists, where they do not)
-    const int ra = 16 * warp + g, rb = ra + 8;
-    const bool working = 16 * warp < rows, has_a = ra < rows, has_b = rb < rows;
-    const long long ma = working ? row_s[has_a ? ra : 0] : 0, mb = working ? row_s[has_b ? rb : 0] : 0;
-    uint4 ha[kSteps16], hb[kSteps16];
-    if (working) {
-        const uint4* H = ws.h + at.part * (pad_rank / 4) + q;
-#pragma unroll
-        for (int k = 0; k < kSteps16; ++k) {
-            ha[k] = hb[k] = make_uint4(0, 0, 0, 0);
-            if (16 * k < rank) {
-                ha[k] = H[ma * quads + 4 * k];
-                hb[k] = H[mb * quads + 4 * k];
-            }
-        }
-    }
-    T* ya = static_cast<T*>(p.y) + ma * p.ldy + at.n0 + 8 * q;
-    T* yb = static_cast<T*>(p.y) + mb * p.ldy + at.n0 + 8 * q;
-    const uint32_t swap = (ra & 1) << 6;   // (rb's is the same)
-    int place = 0;
-    // one tile; `whole`: all of its columns, and all of the rank's steps, exist
-    auto one_tile = [&](int tile, auto whole) {
-        constexpr bool kWhole = decltype(whole)::value;
-        const uint8_t *a_s = smem + place * stage_bytes + ra * 128, *b_s = smem + place * stage_bytes + kManyRows * 128 + g * stride + 8 * q;
-        const int n = tile * kCols;
-#pragma unroll
-        for (int block = 0; block < kBlocks; ++block) {
-            const int cols = kWhole ? 8 : width - n - 32 * block - 8 * q;   // from this lane's first one up to the end
-            Columns<T> va, vb;
-#pragma unroll
-            for (int i = 0; i < 8 / kPieceCols; ++i) {   // (8 columns: one piece of bf16, two of fp32)
-                const uint32_t off = (static_cast<uint32_t>((32 * block + 8 * q) / kPieceCols + i) * 16) ^ swap;
-                va.raw[i] = vb.raw[i] = make_uint4(0, 0, 0, 0);
-                if (cols >= 8) {
-                    va.raw[i] = *reinterpret_cast<const uint4*>(a_s + off);
-                    vb.raw[i] = *reinterpret_cast<const uint4*>(a_s + 8 * 128 + off);
-                }
-            }
-            float acc[4][4];
-            begin_sum<T>(acc, va, 0);
-            begin_sum<T>(acc, vb, 2);
+        // h of rows g and 8 + g of the warp's 16 (of a row that exists, where they do not)
+        const int ra = 16 * warp + g, rb = ra + 8;
+        const bool working = 16 * warp < rows, has_a = ra < rows, has_b = rb < rows;
+        const long long ma = working ? row_s[has_a ? ra : 0] : 0, mb = working ? row_s[has_b ? rb : 0] : 0;
+        uint4 ha[kSteps16], hb[kSteps16];
+        if (working) {
+            const uint4* H = ws.h + at.part * (pad_rank / 4) + q;
 #pragma unroll
             for (int k = 0; k < kSteps16; ++k) {
-                if (!kWhole && 16 * k >= rank) break;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint2 b = *reinterpret_cast<const uint2*>(b_s + (32 * block + 8 * j) * stride + 32 * k);
-                    if (!kWhole && rank - 16 * k < 16) b = masked(b, rank - 16 * k - 4 * q);
-                    mma_bf16(acc[j], ha[k].x, hb[k].x, ha[k].y, hb[k].y, b.x, b.y);
-                    mma_bf16(acc[j], ha[k].z, hb[k].z, ha[k].w, hb[k].w, b.x, b.y);
+                ha[k] = hb[k] = make_uint4(0, 0, 0, 0);
+                if (16 * k < rank) {
+                    ha[k] = H[ma * quads + 4 * k];
+                    hb[k] = H[mb * quads + 4 * k];
                 }
             }
-            if (cols >= 8) {
-                if (has_a) end_sum<T>(acc, va, 0).store(ya + n + 32 * block);
-                if (has_b) end_sum<T>(acc, vb, 2).store(yb + n + 32 * block);
-            } else if (cols > 0) {
-                const T* from = static_cast<const T*>(p.base) + at.n0 + n + 32 * block + 8 * q;
-                if (has_a) add_last<T>(acc, 0, cols, from + ma * p.ldbase, ya + n + 32 * block);
-                if (has_b) add_last<T>(acc, 2, cols, from + mb * p.ldbase, yb + n + 32 * block);
+        }
+        T* ya = static_cast<T*>(p.y) + ma * p.ldy + at.n0 + 8 * q;
+        T* yb = static_cast<T*>(p.y) + mb * p.ldy + at.n0 + 8 * q;
+        const uint32_t swap = (ra & 1) << 6;   // (rb's is the same)
+        int place = 0;
+        // one tile; `whole`: all of its columns, and all of the rank's steps, exist
+        auto one_tile = [&](int tile, auto whole) {
+            constexpr bool kWhole = decltype(whole)::value;
+            const uint8_t *a_s = smem + place * stage_bytes + ra * 128, *b_s = smem + place * stage_bytes + kManyRows * 128 + g * stride + 8 * q;
+            const int n = tile * kCols;
+#pragma unroll
+            for (int block = 0; block < kBlocks; ++block) {
+                const int cols = kWhole ? 8 : width - n - 32 * block - 8 * q;   // from this lane's first one up to the end
+                Columns<T> va, vb;
+#pragma unroll
+                for (int i = 0; i < 8 / kPieceCols; ++i) {   // (8 columns: one piece of bf16, two of fp32)
+                    const uint32_t off = (static_cast<uint32_t>((32 * block + 8 * q) / kPieceCols + i) * 16) ^ swap;
+                    va.raw[i] = vb.raw[i] = make_uint4(0, 0, 0, 0);
+                    if (cols >= 8) {
+                        va.raw[i] = *reinterpret_cast<const uint4*>(a_s + off);
+                        vb.raw[i] = *reinterpret_cast<const uint4*>(a_s + 8 * 128 + off);
+                    }
+                }
+                float acc[4][4];
+                begin_sum<T>(acc, va, 0);
+                begin_sum<T>(acc, vb, 2);
+#pragma unroll
+                for (int k = 0; k < kSteps16; ++k) {
+                    if (!kWhole && 16 * k >= rank) break;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        uint2 b = *reinterpret_cast<const uint2*>(b_s + (32 * block + 8 * j) * stride + 32 * k);
+                        if (!kWhole && rank - 16 * k < 16) b = masked(b, rank - 16 * k - 4 * q);
+                        mma_bf16(acc[j], ha[k].x, hb[k].x, ha[k].y, hb[k].y, b.x, b.y);
+                        mma_bf16(acc[j], ha[k].z, hb[k].z, ha[k].w, hb[k].w, b.x, b.y);
+                    }
+                }
+                if (cols >= 8) {
+                    if (has_a) end_sum<T>(acc, va, 0).store(ya + n + 32 * block);
+                    if (has_b) end_sum<T>(acc, vb, 2).store(yb + n + 32 * block);
+                } else if (cols > 0) {
+                    const T* from = static_cast<const T*>(p.base) + at.n0 + n + 32 * block + 8 * q;
+                    if (has_a) add_last<T>(acc, 0, cols, from + ma * p.ldbase, ya + n + 32 * block);
+                    if (has_b) add_last<T>(acc, 2, cols, from + mb * p.ldbase, yb + n + 32 * block);
+                }
             }
-        }
-    };
+        };
 #pragma unroll 1
-    for (int tile = 0; tile < tiles; ++tile) {
-        copies_wait<kManyStages - 2>();
-        __syncthreads();   // this tile is there for all, and the one before it has been read
-        ask(tile + kManyStages - 1, place == 0 ? kManyStages - 1 : place - 1);
-        if (working) {
-            if (rank == 16 * kSteps16 && (tile + 1) * kCols <= width) one_tile(tile, std::true_type());
-            else one_tile(tile, std::false_type());
+        for (int tile = 0; tile < tiles; ++tile) {
+            copies_wait<kManyStages - 2>();
+            __syncthreads();   // this tile is there for all, and the one before it has been read
+            ask(tile + kManyStages - 1, place == 0 ? kManyStages - 1 : place - 1);
+            if (working) {
+                if (rank == 16 * kSteps16 && (tile + 1) * kCols <= width) one_tile(tile, std::true_type());
+                else one_tile(tile, std::false_type());
+            }
+            place = place == kManyStages - 1 ? 0 : place + 1;
         }
-        place = place == kManyStages - 1 ? 0 : place + 1;
+        copies_wait<0>();
+        __syncthreads();   // (the item's rows and tiles have been read)
     }
-    copies_wait<0>();
 }
 
 // Many rows, high ranks: the tensor core takes its operands from shared memory, and its accumulators are in tensor memory.  Tiles of an item's
@@ -1098,10 +1122,9 @@ cudaError_t launch_kernel(void (*kernel)(Params...), dim3 blocks, int threads, i
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// Lets a kernel use `bytes` of dynamic shared memory, once per device.
 template <class Kernel>
-cudaError_t allow_shared(OncePerDevice& once, Kernel kernel, size_t bytes) {
-    return once([&] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)); });
+cudaError_t allow_shared(Kernel kernel, size_t bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
 }
 struct Passes { int passes, tiles; };   // all ranks, eight at a time, in passes of up to 64
 Passes passes_of(const AdapterParams& p) {
@@ -1113,10 +1136,13 @@ cudaError_t with_tiles(int tiles, F&& f) {
     return tiles == 2 ? f(std::integral_constant<int, 2>()) : tiles == 4 ? f(std::integral_constant<int, 4>())
          : tiles == 6 ? f(std::integral_constant<int, 6>()) : f(std::integral_constant<int, 8>());
 }
-// Pieces of `width` columns of all parts.
-int pieces_of(const AdapterParams& p, int width) {
+// Pieces of `width` columns of all parts; where the kernel looks for them, up to the end of each part too.
+int pieces_of(const AdapterParams& p, int width, int* ends = nullptr) {
     int n = 0;
-    for (int i = 0; i < p.n_parts; ++i) n += (p.part_end[i] - (i ? p.part_end[i - 1] : 0) + width - 1) / width;
+    for (int i = 0; i < kMaxBatch; ++i) {
+        n += (p.part_end[i] - (i ? p.part_end[i - 1] : 0) + width - 1) / width;
+        if (ends) ends[i] = n;
+    }
     return n;
 }
 template <class T, int kRowBytes>
@@ -1124,7 +1150,7 @@ cudaError_t launch_high_y(const AdapterParams& p, int num_sms, cudaStream_t stre
     static OncePerDevice once;
     constexpr int kCols = kRowBytes / sizeof(T);
     const auto kernel = adapters_high_y_kernel<T, kRowBytes>;
-    const cudaError_t e = allow_shared(once, kernel, high_shared(kRowBytes == 512 ? 64 : PRQ_ADAPTER_MAX_RANK, kRowBytes, kCols).total);
+    const cudaError_t e = once([&] { return allow_shared(kernel, high_shared(kRowBytes == 512 ? 64 : PRQ_ADAPTER_MAX_RANK, kRowBytes, kCols).total); });
     if (e != cudaSuccess) return e;
     const int tiles = pieces_of(p, kCols);
     const long long most = static_cast<long long>(tiles) * p.items.n;
@@ -1134,21 +1160,25 @@ template <class T, int kSteps16>
 cudaError_t launch_many_y(const AdapterParams& p, int units, int span, cudaStream_t stream) {
     static OncePerDevice once;
     const auto kernel = adapters_many_y_kernel<T, kSteps16>;
-    const cudaError_t e = allow_shared(once, kernel, kManyStages * many_stage_bytes<T>(PRQ_ADAPTER_MAX_RANK));
+    const cudaError_t e = once([&] { return allow_shared(kernel, kManyStages * many_stage_bytes<T>(16 * kSteps16)); });
     if (e != cudaSuccess) return e;
-    return launch_kernel(kernel, dim3(units * p.items.n), kManyThreads, 1, kManyStages * many_stage_bytes<T>(p.max_rank), stream, p, units, span);
+    return launch_kernel(kernel, dim3(units * p.y_items * p.items.windows), kManyThreads, 1, kManyStages * many_stage_bytes<T>(p.max_rank), stream, p, units, span);
 }
 template <class T>
-cudaError_t launch_few(const AdapterParams& p, cudaStream_t stream) {
+cudaError_t launch_few(AdapterParams p, cudaStream_t stream) {
     const Passes t = passes_of(p);
+    const int units = pieces_of(p, 64, p.unit_end);
     return with_tiles(t.tiles, [&](auto tiles) {
         static OncePerDevice once;
         using Shared = FewShared<decltype(tiles)::value>;
         static_assert(sizeof(Shared) <= 227 * 1024, "shared memory");
-        const auto kernel = adapters_few_kernel<T, decltype(tiles)::value>;
-        const cudaError_t e = allow_shared(once, kernel, sizeof(Shared));
+        const auto kernel = adapters_few_kernel<T, decltype(tiles)::value, true>, looping = adapters_few_kernel<T, decltype(tiles)::value, false>;
+        const cudaError_t e = once([&] {
+            const cudaError_t first = allow_shared(kernel, sizeof(Shared));
+            return first != cudaSuccess ? first : allow_shared(looping, sizeof(Shared));
+        });
         if (e != cudaSuccess) return e;
-        return launch_kernel(kernel, dim3(p.items.n * p.cluster), kHThreads, p.cluster, sizeof(Shared), stream, p, t.passes, pieces_of(p, 64));
+        return launch_kernel(p.h_clusters == p.items.per_window ? kernel : looping, dim3(p.h_clusters * p.items.windows * p.cluster), kHThreads, p.cluster, sizeof(Shared), stream, p, t.passes, units);
     });
 }
 cudaError_t launch_many_h(const AdapterParams& p, cudaStream_t stream) {
@@ -1157,14 +1187,17 @@ cudaError_t launch_many_h(const AdapterParams& p, cudaStream_t stream) {
         static OncePerDevice once;
         using Shared = ManyHShared<decltype(tiles)::value>;
         static_assert(sizeof(Shared) <= 227 * 1024, "shared memory");
-        const auto kernel = adapters_many_h_kernel<decltype(tiles)::value>;
-        const cudaError_t e = allow_shared(once, kernel, sizeof(Shared));
+        const auto kernel = adapters_many_h_kernel<decltype(tiles)::value, true>, looping = adapters_many_h_kernel<decltype(tiles)::value, false>;
+        const cudaError_t e = once([&] {
+            const cudaError_t first = allow_shared(kernel, sizeof(Shared));
+            return first != cudaSuccess ? first : allow_shared(looping, sizeof(Shared));
+        });
         if (e != cudaSuccess) return e;
-        return launch_kernel(kernel, dim3(p.items.n * p.cluster, t.passes), kHThreads, p.cluster, sizeof(Shared), stream, p);
+        return launch_kernel(p.h_clusters == p.items.per_window ? kernel : looping, dim3(p.h_clusters * p.items.windows * p.cluster, t.passes), kHThreads, p.cluster, sizeof(Shared), stream, p);
     });
 }
 template <class T>
-cudaError_t launch_many_y(const AdapterParams& p, int num_sms, cudaStream_t stream) {
+cudaError_t launch_many_y(AdapterParams p, int num_sms, cudaStream_t stream) {
     // Tensor memory for ranks above 32 where a CTA has many tiles (gate / up of 4096 tokens, 16 tiles of 256 columns per SM: rank 64 125 us
     // with mma.sync, 105 so; rank 32 84 and 98; q / k / v, five per SM: rank 64 68 either way, rank 32 42 and 54; 1024 tokens of gate / up,
     // rank 64: 47 either way), and for ranks above 64, whose h mma.sync's registers do not hold.
@@ -1172,9 +1205,9 @@ cudaError_t launch_many_y(const AdapterParams& p, int num_sms, cudaStream_t stre
     if (p.pad_rank > 64) return launch_high_y<T, 256>(p, num_sms, stream);
     if (p.pad_rank > 32 && static_cast<long long>(pieces_of(p, 512 / sizeof(T))) * items >= 8ll * num_sms) return launch_high_y<T, 512>(p, num_sms, stream);
     // a CTA's tiles: one where there are few of them, up to four for less to set up
-    const int span = static_cast<int>(std::max<long long>(1, std::min<long long>(4, static_cast<long long>(pieces_of(p, kManyCols<T>)) * items / (6ll * num_sms))));
-    const int units = pieces_of(p, kManyCols<T> * span), steps = p.pad_rank / 16;
-    if (static_cast<long long>(units) * p.items.n > 0x7fffffffll) return cudaErrorInvalidValue;
+    int span = static_cast<int>(std::max<long long>(1, std::min<long long>(4, static_cast<long long>(pieces_of(p, kManyCols<T>)) * items / (6ll * num_sms))));
+    while (static_cast<long long>(pieces_of(p, kManyCols<T> * span)) * p.y_items * p.items.windows > 0x7fffffffll) span *= 2;   // (a grid's limit)
+    const int units = pieces_of(p, kManyCols<T> * span, p.unit_end), steps = p.pad_rank / 16;
     return steps == 1 ? launch_many_y<T, 1>(p, units, span, stream) : steps == 2 ? launch_many_y<T, 2>(p, units, span, stream) : launch_many_y<T, 4>(p, units, span, stream);
 }
 
@@ -1182,27 +1215,38 @@ cudaError_t launch_many_y(const AdapterParams& p, int num_sms, cudaStream_t stre
 
 size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank) {
     const AdapterItems items = plan_items(M, n_slots);
-    if (M <= kFewCall) return 0;
+    if (small_items(M, n_slots)) return 0;
     const size_t ranks = n_parts * ((max_rank + 15) & ~15);
-    return items.n < 0 ? 0 : counts_bytes(items) + sizeof(Item) * items.n + 4 * ranks * static_cast<size_t>(M);
+    return counts_bytes(items) + sizeof(Item) * items.n + 4 * ranks * static_cast<size_t>(M);
 }
 
 cudaError_t launch_adapters(const AdapterParams& in, bool bf16, int num_sms, cudaStream_t stream, int* launches) {
     AdapterParams p = in;
     p.items = plan_items(p.M, p.n_slots);
     p.pad_rank = (p.max_rank + 15) & ~15;
-    if (p.items.n < 1) return cudaErrorInvalidValue;
-    const bool few = p.M <= kFewCall;
+    const bool few = small_items(p.M, p.n_slots);
     const int passes = few ? 1 : passes_of(p).passes;
     const int full = p.M / kManyRows, items = few ? p.items.n : full + std::min(p.n_slots, full) / 4 + 1;
+    // CTAs of a cluster: as many as let all items (of large ones, those of the rows, and of some more adapters) be on the GPU at once, with 8
+    // steps of K each (4 for many rows), and of small items with an adapter of 640 KB per CTA and more in any case (q / k / v of rank 64, 200
+    // rows of a pool of 64, four of them in use: 64 us without that, 38 so; all in use: 76 and 46).
     p.cluster = 1;
-    for (int c = 2; c <= 8; ++c)
-        if (static_cast<long long>(items) * passes * c <= num_sms / 18 * (18 / c) * c && p.K / 32 >= (few ? 8 : 4) * c) p.cluster = c;
+    const long long bytes = 2ll * p.pad_rank * (static_cast<long long>(p.n_parts) * p.K + p.N), sixth = num_sms / 18;
+    for (int c = 2; c <= 8; ++c) {
+        const bool at_once = static_cast<long long>(items) * passes * c <= sixth * (18 / c) * c;
+        if ((at_once || (few && bytes >= 655360ll * c)) && p.K / 32 >= (few ? 8 : 4) * c) p.cluster = c;
+    }
+    // How many items there are is not known here, and a pool of 64 may be used by four adapters: clusters, and CTAs of y, for as many items as
+    // run at once, each with every so many-th one.  (1000 rows of a pool of 64, four in use: 18 us, with a cluster for each item that there
+    // could be 36; pool of 500: 18 and 193.)
+    const int windows = p.items.windows, whole = p.items.window / kManyRows;
+    p.h_clusters = std::min(p.items.per_window, static_cast<int>(std::max<long long>(1, (sixth * (18 / p.cluster) / passes + windows - 1) / windows)));
     if (few) {
         const cudaError_t e = bf16 ? launch_few<__nv_bfloat16>(p, stream) : launch_few<float>(p, stream);
         *launches = e == cudaSuccess;
         return e;
     }
+    p.y_items = std::min(p.items.per_window, whole + whole / 4 + 8);
     cudaError_t e = launch_many_h(p, stream);
     if (e != cudaSuccess) return e;
     ++*launches;

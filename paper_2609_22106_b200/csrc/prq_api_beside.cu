@@ -11,6 +11,8 @@ using namespace prq;
 
 namespace {
 
+constexpr int kMaxAdapterRows = 1 << 23;   // (items, and with them grids, stay within 31 bits)
+
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // A description as it is used: fields checked, sums done.
@@ -57,7 +59,7 @@ prq_status rotate(const prq_rope* r, const int32_t* positions, int M, const prq_
     for (int i = 0; i < 2; ++i) {
         if (!in[i] || in[i]->heads == 0) continue;
         const prq_heads& h = *in[i];
-        if (h.heads < 0 || h.heads > (1 << 20) || !h.x || !h.out) return PRQ_ERR_INVALID_ARG;
+        if (h.heads < 0 || h.heads > (1 << 16) || !h.x || !h.out) return PRQ_ERR_INVALID_ARG;
         // results on top of one another (that no row meets another row's heads is the caller's part: any order of strides is open)
         if ((h.heads > 1 && std::llabs(h.hsout) < r->head_dim) || (M > 1 && std::llabs(h.ldout) < r->head_dim)) return PRQ_ERR_INVALID_ARG;
         if (h.x == h.out && (h.ldx != h.ldout || h.hsx != h.hsout)) return PRQ_ERR_INVALID_ARG;
@@ -90,7 +92,7 @@ extern "C" {
 
 size_t prq_adapters_workspace_bytes(const prq_adapters* a, int M) {
     AdapterParams p;
-    if (M < 1 || read_adapters(a, &p) != PRQ_OK) return 0;
+    if (M < 1 || M >= kMaxAdapterRows || read_adapters(a, &p) != PRQ_OK) return 0;
     return adapters_workspace_bytes(M, p.n_slots, p.n_parts, p.max_rank);
 }
 
@@ -101,7 +103,7 @@ prq_status prq_linear_adapters(const prq_adapters* a, const int32_t* row_adapter
     prq_status st = read_adapters(a, &p);
     if (st != PRQ_OK) return st;
     if (M == 0) return PRQ_OK;
-    if (M < 0 || (y_dtype != PRQ_F32 && y_dtype != PRQ_BF16) || !row_adapter || !x || !base || !y || !p.A || !p.B) return PRQ_ERR_INVALID_ARG;
+    if (M < 0 || M >= kMaxAdapterRows || (y_dtype != PRQ_F32 && y_dtype != PRQ_BF16) || !row_adapter || !x || !base || !y || !p.A || !p.B) return PRQ_ERR_INVALID_ARG;
     if (ldx < p.K || ldbase < p.N || ldy < p.N || (base == y && ldbase != ldy)) return PRQ_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(base) || !aligned16(y) || !aligned16(p.A) || !aligned16(p.B)) return PRQ_ERR_ALIGNMENT;
     const int unit = y_dtype == PRQ_F32 ? 4 : 8;

@@ -244,10 +244,10 @@ struct AdapterParams {
     int M, K, N, n_slots, max_rank, n_parts;
     int cluster;                 // CTAs per cluster
     int pad_rank;                // max_rank in whole k steps of 16
-    int y_size;                  // bytes of an element of base and y
-    uint32_t base_ahead;         // bytes of each row of base that are asked for in L2 ahead
     AdapterItems items;
+    int h_clusters, y_items;     // clusters, and groups of CTAs, per window: each has every so many-th item
     int part_end[kMaxBatch];     // column behind each part
+    int unit_end[kMaxBatch];     // pieces of columns up to the end of each part, as the launch cuts them
 };
 size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank);
 cudaError_t launch_adapters(const AdapterParams& p, bool bf16, int num_sms, cudaStream_t stream, int* launches);

@@ -83,3 +83,25 @@ def heads(t, positions, f, factor, rot, layout, norm=False, weight=None, eps=1e-
     off[..., first] = both
     off[..., second] = both
     return r, off + half_step(t.dtype) * (r.abs() + off) + 1e-37
+
+
+def adapters_of_many(x, A, B, parts, rows, base, scale=None, ranks=None):
+    """The same for many rows: a matrix product in 64 bits per adapter."""
+    S, P, R, K = A.shape
+    y, off = base.double().clone(), torch.zeros(base.shape, dtype=torch.float64, device=base.device)
+    for a in rows.unique().tolist():
+        if not 0 <= a < S:
+            continue
+        at = torch.nonzero(rows == a).flatten()
+        rank = R if ranks is None else min(max(int(ranks[a]), 0), R)
+        s = 1.0 if scale is None else float(scale[a])
+        begin = 0
+        for p, n in enumerate(parts):
+            xd, w = x[at].double(), A[a, p, :rank].double().T
+            h, hs = xd @ w, xd.abs() @ w.abs()
+            b = B[a, begin:begin + n, :rank].double().T
+            e = 2 * U * (K + 8) * hs + 2.0 ** -16 * h.abs() + 2 * U * (R + 8) * h.abs()
+            y[at, begin:begin + n] += s * (h @ b)
+            off[at, begin:begin + n] = abs(s) * (e @ b.abs()) * (1 + 2.0 ** -10)
+            begin += n
+    return y, off + (half_step(base.dtype) + 2 * U) * (y.abs() + off)

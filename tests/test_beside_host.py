@@ -111,6 +111,18 @@ def test_adapters_refused_without_a_workspace_or_a_pool(fake):  # noqa: F811
     assert fake.lib().prq_adapters_workspace_bytes(ctypes.addressof(p), 0) == 0 and fake.lib().prq_adapters_workspace_bytes(None, 3) == 0
 
 
+def test_adapters_workspace_by_rows_and_slots(fake):  # noqa: F811
+    def need(M, **f):
+        pool = _pool(fake, **f)
+        return fake.lib().prq_adapters_workspace_bytes(ctypes.addressof(pool), M)
+
+    assert need(128) == 0 and need(129) > 129 * 2 * 16 * 4 and need(129, S=64) == 0 and need(1024, S=64) > 0 and need(1 << 20, S=600) == 0
+    assert need(5000) > need(4096) and need((1 << 23) - 1) > (1 << 23) * 2 * 16 * 4 - 1024 and need(1 << 23) == 0
+    big = _pool(fake)
+    assert _call(fake, big, M=1 << 23) == 1 and _call(fake, big, M=129, bytes=need(129) - 1) == 8 and _call(fake, big, M=129, ws=None) == 8
+    assert _call(fake, big, M=129, ws=_aligned(1 << 20).ctypes.data + 8) == 2 and _call(fake, big, M=129) == 0 and _call(fake, _pool(fake, S=64), M=129, ws=None, bytes=0) == 0
+
+
 def _heads(fake, x=1, out=1, ldx=256, hsx=64, ldout=256, hsout=64, heads=4, weight=0):  # noqa: F811
     some = _aligned(16).ctypes.data
     at = lambda v: some if v == 1 else v
@@ -147,3 +159,8 @@ def test_heads_refused(fake, status, q, call):  # noqa: F811
     if "x" not in q and not call:
         assert _rotate(fake, _heads(fake), _heads(fake, **q), **call) == (status, 0)
     assert _rotate(fake, None) == (1, 0)
+
+
+def test_more_heads_than_a_row_can_have(fake):  # noqa: F811
+    assert _rotate(fake, _heads(fake, heads=65536, ldx=1 << 23, ldout=1 << 23)) == (0, 1)
+    assert _rotate(fake, _heads(fake, heads=65537, ldx=1 << 23, ldout=1 << 23)) == (1, 0)
