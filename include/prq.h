@@ -429,9 +429,9 @@ typedef struct prq_adapters {
                                     adapter's rank is not used (it may be anything, NaN among it)                */
 } prq_adapters;
 
-/* Scratch of one prq_linear_adapters call for M rows; it need not be cleared, and calls that may overlap need one each.
- * Returns 0 for invalid arguments, and where none is needed: up to 128 rows, and up to 16 rows per slot
- * of the pool. */
+/* Scratch of one prq_linear_adapters call for up to M rows; it need not be cleared, and calls that may overlap need one each.
+ * Returns 0 for invalid arguments, and where none is needed: among others for up to 512 rows of a pool
+ * whose parts' ranks (max_rank in whole 16s, n_parts times) are 64 at most. */
 size_t prq_adapters_workspace_bytes(const prq_adapters *a, int M);
 
 /*   row_adapter  device, M int32: each row's slot.  A row whose entry is not in [0, n_slots) -- -1, say -- has no adapter.  Rows

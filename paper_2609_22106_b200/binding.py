@@ -559,7 +559,7 @@ def _load_torch():
 
 
 ADAPTER_MAX_RANK = 128
-ADAPTER_FEW_ROWS = 128   # rows of a call that needs no workspace
+ADAPTER_FEW_ROWS, ADAPTER_FEW_RANKS = 512, 64   # up to that many rows, and ranks of all parts in whole 16s, a call needs no workspace
 
 
 class AdapterPool(ctypes.Structure):
@@ -586,6 +586,7 @@ class Adapters:
         _require(all(t is None or t.get_device() == A.get_device() for t in (B, scale, ranks)) and A.is_cuda, where)
         self.A, self.B, self.scale, self.ranks, self.parts, self.N, self.K = A, B, scale, ranks, parts, sum(parts), K
         self.device = A.get_device()
+        self._free_rows = ADAPTER_FEW_ROWS if P * ((R + 15) // 16 * 16) <= ADAPTER_FEW_RANKS else 0
         self._pool = AdapterPool(ctypes.sizeof(AdapterPool), S, R, K, P, (ctypes.c_int * 4)(*parts), _dptr(A), _dptr(B), _dptr(scale), _dptr(ranks))
         self._p = ctypes.addressof(self._pool)
 
@@ -623,7 +624,7 @@ def linear_adapters(adapters: Adapters, x, row_adapter, base, out=None, workspac
         ldx, ldbase = K, (N + 7) // 8 * 8
         ldout = ldbase
     if workspace is None:
-        if M > ADAPTER_FEW_ROWS:
+        if M > adapters._free_rows:
             if stream is None:
                 workspace = adapters_workspace(adapters, M)
             else:   # from the memory of the call's stream

@@ -68,7 +68,7 @@ struct Columns {
 // ---------------------------------------------------------------- items
 // Up to 16 rows each, or up to 128, so that A and B are read seldom and h and y have whole tiles.
 constexpr int kFewRows = 16, kManyRows = 128;
-constexpr int kFewCall = 128;         // rows of a call up to which items are small in any case
+constexpr int kFewCall = 512;         // rows of a call up to which items are small where one pass takes all ranks
 constexpr int kWindow = 4096;         // rows that are put in the order of their adapters together
 constexpr int kSortedSlots = 511;     // pools of more adapters, and calls of up to 32 rows: 32 rows that follow one another are grouped
 
@@ -77,12 +77,23 @@ struct __align__(16) Item {
     int row[kManyRows];
 };
 
-// Small items where adapters may have fewer rows than such an item, too.  (q / k / v, rank 16, 1000 rows of a pool of 64: all of them in use
-// 23 us, with large items 80; four of them in use 23 and 18.  Pool of 500: 102 and 582, 23 and 18.  Pool of 4: 15 and 18, but rank 64 39 and 27.
-// Rank 64, 200 rows of a pool of 64: 46 and 130, four in use 38 and 14.)  And where rows are put in order 32 at a time.
-bool small_items(int M, int n_slots) { return M <= kFewCall || n_slots > kSortedSlots || M < kFewRows * n_slots; }
+constexpr int kItemsSoon = 24;        // items times passes that clusters of eight CTAs work off in two turns
+// All ranks of all parts are summed in passes of up to 64, which small items take one after another and large ones at the same time.
+int passes_of(int n_parts, int max_rank) { return (n_parts * ((max_rank + 15) & ~15) + 63) / 64; }
+// Small items and one launch, or large ones and two.  One pass: small up to 512 rows (o of 387 rows, rank 32: 10.1 us, with large items 12.0;
+// gate / up of 512 rows, rank 16: 21 and 20; of 768: 28 and 21), and wherever adapters may have fewer rows than such an item (q / k / v, rank 16, 1000
+// rows of a pool of 64: all of them in use 23 and 80, four in use 23 and 18; of a pool of 500 102 and 582, 23 and 18).  Several passes: large where
+// there cannot be more items than clusters work off soon (q / k / v, rank 64, one row: 9.1 and 17 with a small item; 48 rows of a pool of 4: 10 to 12
+// and 21; of 8: 11 to 21 and 21), small where adapters may have few rows (200 rows of a pool of 64: all in use 46 and 130, four in use 38 and 14;
+// 256 of a pool of 32: 36 and 71, 36 and 16).  And small where rows are put in order 32 at a time.
+bool small_items(int M, int n_slots, int passes) {
+    const long long room = static_cast<long long>(kFewRows) * n_slots;
+    if (n_slots > kSortedSlots) return true;
+    if (passes == 1) return M <= kFewCall || M < room;
+    return (M < n_slots ? M : n_slots) * passes > kItemsSoon && M < room;
+}
 // rows per window, items that a window may have, windows, items in all
-AdapterItems plan_items(int M, int n_slots) {
+AdapterItems plan_items(int M, int n_slots, bool small) {
     AdapterItems t;
     if (n_slots > kSortedSlots) {
         t.window = M < 32 ? M : 32;
@@ -90,7 +101,7 @@ AdapterItems plan_items(int M, int n_slots) {
     } else {
         t.window = M < kWindow ? M : kWindow;
         const int kinds = n_slots + 1 < t.window ? n_slots + 1 : t.window;
-        t.per_window = t.window / (small_items(M, n_slots) ? kFewRows : kManyRows) + kinds;   // whole ones, and a rest of each adapter
+        t.per_window = t.window / (small ? kFewRows : kManyRows) + kinds;   // whole ones, and a rest of each adapter
     }
     t.windows = static_cast<int>((M + static_cast<long long>(t.window) - 1) / t.window);
     t.n = t.windows * t.per_window;   // (under 2^23 rows: 31 bits hold that, and all grids)
@@ -377,7 +388,10 @@ __device__ __forceinline__ uint4 two_terms(float4 sum, float scale, int r, int r
     return h;
 }
 
-// Many rows: h of an item goes to the workspace, for the second launch.
+// Many rows: h of an item goes to the workspace, for the second launch.  4096 rows of q / k / v (K = 2560), rank 16: 15 us, of which the loop over
+// K takes 7 (21 MB of x), finding the rows 2.4, set-up 1, the first loads 1.6, the cluster's exchange 3.  Every CTA pushes its sums to
+// the one that adds them up; fetching them took 2 us more.
+// kOnce: there is a cluster for each item that there could be.  (The loop over items costs registers: 0.3 to 0.6 us per call.)
 template <int kRankTiles>
 struct ManyHShared : HShared<kRankTiles, kManyRows> {
     float4 got[kManyRows * 8 * kRankTiles / 4 + 8];   // sums of the cluster's CTAs for this CTA's share of them, one CTA behind the other
@@ -516,6 +530,8 @@ __device__ __forceinline__ void copy_rows(const AdapterParams& p, const int* row
 }
 
 // Few rows: one launch.  Every CTA of an item's cluster gets all of its sums, and a share of the columns: 64 per warp, straight from memory.
+// Bound by a chain of latencies, not by bytes: one row of q / k / v, rank 16, 6.9 us (finding it 1, loads of x and A 2, exchange 1, loads of
+// B and base, products and stores 2); 64 rows with 58 adapters 15.8 us, 27 MB.  Two launches took 7.1 and 18.9.
 template <int kRankTiles>
 struct FewShared : HShared<kRankTiles, kFewRows> {
     uint4 h[kFewRows * PRQ_MULTI_MAX * PRQ_ADAPTER_MAX_RANK / 4];   // [rank / 4][row]
@@ -640,7 +656,8 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_few_kernel(const __grid
     }
 }
 
-// Many rows: a CTA has an item and `span` tiles of kCols columns of one part.  Tiles of base and B come into a ring in shared memory; a
+// Many rows: a CTA has every y_items-th item of a window, and `span` tiles of kCols columns of one part.  Bound by memory: 4096 rows of
+// q / k / v in place, rank 16, 25 us for 101 MB, 4 TB/s (a copy in place of that pattern takes 20 to 22).  Tiles of base and B come into a ring in shared memory; a
 // warp has 16 of the item's rows, whose h it keeps in registers, and all columns.  In the ring a row of B stands where the fragment's
 // lane wants it (row n of a block of 32 at 8 ((n % 8) / 2) + 2 (n / 8) + n % 2), with a stride of 32 bytes off a multiple of 64; of base,
 // odd rows have the halves of their 128 bytes swapped: no lane of a load meets another one's bank.
@@ -798,6 +815,8 @@ __global__ void __launch_bounds__(kManyThreads, kSteps16 == 1 ? 3 : 2) adapters_
 // row, which neighbouring threads copy, stay within 128 bytes.  (Without swizzle each goes to a line of shared memory of its own, and
 // the copies of one tile of B took 2500 cycles instead of 300.)  Rows of base: piece i of row r (16 bytes) at
 // i ^ (r & 7), so that eight threads with a row each meet no bank twice.
+// Bound by shared memory, which a tile passes five times (base and B in, operands, base again, and out): 4096 rows of gate / up in place, rank
+// 64, 87 us for 319 MB, 3.7 TB/s; with fragments from shared memory (mma.sync) 110.
 constexpr int kHighThreads = 512, kHighWarps = kHighThreads / 32;
 struct HighShared { int k_bytes, blocks, h, base, b, total; };   // bytes of K per row, blocks of them; bytes of h, a tile of base, of B, and in all, with two of each tile
 __host__ __device__ inline HighShared high_shared(int pad_rank, int row_bytes, int cols) {
@@ -1126,9 +1145,9 @@ template <class Kernel>
 cudaError_t allow_shared(Kernel kernel, size_t bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
 }
-struct Passes { int passes, tiles; };   // all ranks, eight at a time, in passes of up to 64
+struct Passes { int passes, tiles; };   // tiles: eights of ranks per pass
 Passes passes_of(const AdapterParams& p) {
-    const int ranks = p.n_parts * p.pad_rank, passes = (ranks + 63) / 64, tiles = (ranks / 8 + passes - 1) / passes;
+    const int passes = passes_of(p.n_parts, p.max_rank), tiles = (p.n_parts * p.pad_rank / 8 + passes - 1) / passes;
     return Passes{passes, tiles <= 2 ? 2 : tiles <= 4 ? 4 : tiles <= 6 ? 6 : 8};
 }
 template <class F>
@@ -1204,7 +1223,8 @@ cudaError_t launch_many_y(AdapterParams p, int num_sms, cudaStream_t stream) {
     const int items = (p.M + kManyRows - 1) / kManyRows;
     if (p.pad_rank > 64) return launch_high_y<T, 256>(p, num_sms, stream);
     if (p.pad_rank > 32 && static_cast<long long>(pieces_of(p, 512 / sizeof(T))) * items >= 8ll * num_sms) return launch_high_y<T, 512>(p, num_sms, stream);
-    // a CTA's tiles: one where there are few of them, up to four for less to set up
+    // a CTA's tiles: one where there are few of them, up to four for less to set up (q / k / v of 4096 rows, rank 16: 41 us with four, 48 with
+    // one, 45 with eight; o of 387 rows, rank 32: 13.1 with one, 14.9 with four)
     int span = static_cast<int>(std::max<long long>(1, std::min<long long>(4, static_cast<long long>(pieces_of(p, kManyCols<T>)) * items / (6ll * num_sms))));
     while (static_cast<long long>(pieces_of(p, kManyCols<T> * span)) * p.y_items * p.items.windows > 0x7fffffffll) span *= 2;   // (a grid's limit)
     const int units = pieces_of(p, kManyCols<T> * span, p.unit_end), steps = p.pad_rank / 16;
@@ -1213,19 +1233,22 @@ cudaError_t launch_many_y(AdapterParams p, int num_sms, cudaStream_t stream) {
 
 }  // namespace
 
-size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank) {
-    const AdapterItems items = plan_items(M, n_slots);
-    if (small_items(M, n_slots)) return 0;
+size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank, bool any_fewer) {
+    // (several passes: a few rows need some where a middling number does not)
+    if (any_fewer) return std::max(adapters_workspace_bytes(M, n_slots, n_parts, max_rank, false),
+                                   adapters_workspace_bytes(std::max(1, std::min(M, kItemsSoon / passes_of(n_parts, max_rank))), n_slots, n_parts, max_rank, false));
+    if (small_items(M, n_slots, passes_of(n_parts, max_rank))) return 0;
+    const AdapterItems items = plan_items(M, n_slots, false);
     const size_t ranks = n_parts * ((max_rank + 15) & ~15);
     return counts_bytes(items) + sizeof(Item) * items.n + 4 * ranks * static_cast<size_t>(M);
 }
 
 cudaError_t launch_adapters(const AdapterParams& in, bool bf16, int num_sms, cudaStream_t stream, int* launches) {
     AdapterParams p = in;
-    p.items = plan_items(p.M, p.n_slots);
     p.pad_rank = (p.max_rank + 15) & ~15;
-    const bool few = small_items(p.M, p.n_slots);
-    const int passes = few ? 1 : passes_of(p).passes;
+    const bool few = small_items(p.M, p.n_slots, passes_of(p.n_parts, p.max_rank));
+    const int passes = few ? 1 : passes_of(p.n_parts, p.max_rank);
+    p.items = plan_items(p.M, p.n_slots, few);
     const int full = p.M / kManyRows, items = few ? p.items.n : full + std::min(p.n_slots, full) / 4 + 1;
     // CTAs of a cluster: as many as let all items (of large ones, those of the rows, and of some more adapters) be on the GPU at once, with 8
     // steps of K each (4 for many rows), and of small items with an adapter of 640 KB per CTA and more in any case (q / k / v of rank 64, 200

@@ -93,7 +93,7 @@ extern "C" {
 size_t prq_adapters_workspace_bytes(const prq_adapters* a, int M) {
     AdapterParams p;
     if (M < 1 || M >= kMaxAdapterRows || read_adapters(a, &p) != PRQ_OK) return 0;
-    return adapters_workspace_bytes(M, p.n_slots, p.n_parts, p.max_rank);
+    return adapters_workspace_bytes(M, p.n_slots, p.n_parts, p.max_rank, true);
 }
 
 prq_status prq_linear_adapters(const prq_adapters* a, const int32_t* row_adapter, const void* x, int M, int ldx, const void* base, int ldbase,
@@ -110,7 +110,7 @@ prq_status prq_linear_adapters(const prq_adapters* a, const int32_t* row_adapter
     if (ldx % 8 || ldbase % unit || ldy % unit) return PRQ_ERR_ALIGNMENT;
     for (const void* v : {static_cast<const void*>(row_adapter), static_cast<const void*>(p.scale), static_cast<const void*>(p.ranks)})
         if (reinterpret_cast<uintptr_t>(v) % 4) return PRQ_ERR_ALIGNMENT;
-    const size_t need = adapters_workspace_bytes(M, p.n_slots, p.n_parts, p.max_rank);
+    const size_t need = adapters_workspace_bytes(M, p.n_slots, p.n_parts, p.max_rank, false);
     if (need) {
         if (!workspace || workspace_bytes < need) return PRQ_ERR_WORKSPACE;
         if (!aligned16(workspace)) return PRQ_ERR_ALIGNMENT;

@@ -249,7 +249,7 @@ struct AdapterParams {
     int part_end[kMaxBatch];     // column behind each part
     int unit_end[kMaxBatch];     // pieces of columns up to the end of each part, as the launch cuts them
 };
-size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank);
+size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank, bool any_fewer);   // any_fewer: enough for up to M rows
 cudaError_t launch_adapters(const AdapterParams& p, bool bf16, int num_sms, cudaStream_t stream, int* launches);
 
 // Benchmark utility: `grid` CTAs each issuing n_mma block-scaled FP4 MMAs (128 x 256 x 64) from shared memory.

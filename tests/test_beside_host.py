@@ -116,11 +116,12 @@ def test_adapters_workspace_by_rows_and_slots(fake):  # noqa: F811
         pool = _pool(fake, **f)
         return fake.lib().prq_adapters_workspace_bytes(ctypes.addressof(pool), M)
 
-    assert need(128) == 0 and need(129) > 129 * 2 * 16 * 4 and need(129, S=64) == 0 and need(1024, S=64) > 0 and need(1 << 20, S=600) == 0
+    assert need(512) == 0 and need(513) > 513 * 2 * 16 * 4 and need(513, S=64) == 0 and need(1024, S=64) > 0 and need(1 << 20, S=600) == 0
+    assert need(1, R=64) > 2 * 64 * 4 and all(need(M + 1, R=R, S=S) >= need(M, R=R, S=S) for R in (40, 64, 128) for S in (1, 2, 8, 64) for M in range(1, 600))   # up to M rows
     assert need(5000) > need(4096) and need((1 << 23) - 1) > (1 << 23) * 2 * 16 * 4 - 1024 and need(1 << 23) == 0
     big = _pool(fake)
-    assert _call(fake, big, M=1 << 23) == 1 and _call(fake, big, M=129, bytes=need(129) - 1) == 8 and _call(fake, big, M=129, ws=None) == 8
-    assert _call(fake, big, M=129, ws=_aligned(1 << 20).ctypes.data + 8) == 2 and _call(fake, big, M=129) == 0 and _call(fake, _pool(fake, S=64), M=129, ws=None, bytes=0) == 0
+    assert _call(fake, big, M=1 << 23) == 1 and _call(fake, big, M=513, bytes=need(513) - 1) == 8 and _call(fake, big, M=513, ws=None) == 8
+    assert _call(fake, big, M=513, ws=_aligned(1 << 20).ctypes.data + 8) == 2 and _call(fake, big, M=513) == 0 and _call(fake, _pool(fake, S=64), M=513, ws=None, bytes=0) == 0
 
 
 def _heads(fake, x=1, out=1, ldx=256, hsx=64, ldout=256, hsout=64, heads=4, weight=0):  # noqa: F811

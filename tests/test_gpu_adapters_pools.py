@@ -69,6 +69,26 @@ def test_pools_of_many_adapters(prq, M, K, parts, R, S, used, dtype):
     _both_ways(prq, x, A, B, parts, rows, base)
 
 
+@pytest.mark.parametrize("M", [1, 2, 3, 4, 5, 6, 7, 12, 13, 16, 42, 43])
+@pytest.mark.parametrize("R,parts", [(64, [128, 64, 64]), (128, [72, 33]), (40, [64, 64]), (24, [1040, 16, 8, 5])])
+def test_few_rows_of_high_ranks(prq, M, R, parts):
+    """On both sides of where a call changes from one launch to two."""
+    K, S = 2560, 8
+    g, x, A, B, base = _inputs(M + R, M, K, parts, R, S, "bf16")
+    ranks = torch.tensor([R, R - 1, 0, 1, 17, R, 8, R], dtype=torch.int32, device="cuda")
+    for pattern in ("mix", "some"):
+        _both_ways(prq, x, A, B, parts, _rows(pattern, M, S, g), base, scale=torch.rand(S, generator=g, device="cuda") * 2 - 0.5, ranks=ranks)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,S", [(511, 4), (512, 4), (513, 4), (1023, 64), (1024, 64), (31, 511), (33, 512)])
+def test_where_the_form_changes(prq, M, S, dtype):
+    parts, K, R = [200, 33], 1056, 16
+    g, x, A, B, base = _inputs(M + S, M, K, parts, R, S, dtype)
+    for pattern in ("mix", "some", "sorted"):
+        _both_ways(prq, x, A, B, parts, _rows(pattern, M, S, g), base)
+
+
 @pytest.mark.parametrize("M,S,R", [(300, 64, 16), (1000, 30, 64), (1100, 8, 128)])
 def test_a_captured_call_finds_more_items_than_it_had(prq, M, S, R):
     """Captured with one adapter in use, replayed with all of them, and with none."""
