@@ -171,7 +171,7 @@ struct Unit {
         const int lane = threadIdx.x & 31;
         u = lane % kLanes;
         g = lane / kLanes;
-        inside = u < p.head_dim / 16;
+        inside = u < p.head_dim / 16 && g < 32 / kLanes;
         rotated = u < p.rot_dim / 16;
         ea = kInterleaved || !rotated ? 16 * u : 8 * u;   // (what does not turn begins at 16 units of what does)
         eb = kInterleaved || !rotated ? ea + 8 : ea + p.rot_dim / 2;
@@ -231,22 +231,28 @@ struct Unit {
     }
 };
 
-// Cosines and sines of a row's pairs, a pair a thread; `mine` is the thread's first one.
-template <int kPairs>
-__device__ __forceinline__ void turn_pairs(const RotateParams& p, uint64_t mine, int pos, float (&angle)[2][kPairs]) {
+// Cosines and sines of a row's pairs, a pair a thread; `mine` is the thread's first one.  A unit's eight pairs lie in two fours, next to those
+// of the other units: a warp's 16-byte loads meet no bank twice.
+template <int kLanes>
+using Angles = float[4][kLanes][4];   // cosines of pairs 0 .. 3 of every unit, of pairs 4 .. 7, sines of both
+template <int kLanes>
+__device__ __forceinline__ void turn_pairs(const RotateParams& p, uint64_t mine, int pos, Angles<kLanes>& angle) {
     for (int i = threadIdx.x; i < p.rot_dim / 2; i += blockDim.x) {
         float c, s;
         cos_sin((i == static_cast<int>(threadIdx.x) ? mine : p.turns[i]) * static_cast<uint64_t>(static_cast<int64_t>(pos)), &c, &s);
-        angle[0][i] = c * p.factor;
-        angle[1][i] = s * p.factor;
+        angle[i >> 2 & 1][i >> 3][i & 3] = c * p.factor;
+        angle[2 + (i >> 2 & 1)][i >> 3][i & 3] = s * p.factor;
     }
 }
-template <int kPairs>
-__device__ __forceinline__ void read_pairs(const float (&angle)[2][kPairs], int u, f32x2 (&c)[4], f32x2 (&s)[4]) {
+template <int kLanes>
+__device__ __forceinline__ void read_pairs(const Angles<kLanes>& angle, int u, f32x2 (&c)[4], f32x2 (&s)[4]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        c[j] = *reinterpret_cast<const f32x2*>(&angle[0][8 * u + 2 * j]);
-        s[j] = *reinterpret_cast<const f32x2*>(&angle[1][8 * u + 2 * j]);
+    for (int j = 0; j < 2; ++j) {
+        const ulonglong2 vc = *reinterpret_cast<const ulonglong2*>(angle[j][u]), vs = *reinterpret_cast<const ulonglong2*>(angle[2 + j][u]);
+        c[2 * j] = vc.x;
+        c[2 * j + 1] = vc.y;
+        s[2 * j] = vs.x;
+        s[2 * j + 1] = vs.y;
     }
 }
 
@@ -258,7 +264,7 @@ __device__ __forceinline__ void read_pairs(const float (&angle)[2][kPairs], int 
 template <class T, bool kInterleaved, bool kNorm, int kLanes, int kTimes>
 __global__ void __launch_bounds__(kRotateWarps * 32, 3) rotate_kernel(const __grid_constant__ RotateParams p, int warps_q) {
     constexpr int kHeads = 32 / kLanes;
-    __shared__ __align__(16) float angle_s[2][kLanes * 8];
+    __shared__ __align__(16) Angles<kLanes> angle_s;
     Unit<T, kInterleaved, kNorm, kLanes> unit(p);
     const int warp = blockIdx.y * (blockDim.x >> 5) + (threadIdx.x >> 5);
     const bool key = warp >= warps_q;
@@ -283,10 +289,10 @@ __global__ void __launch_bounds__(kRotateWarps * 32, 3) rotate_kernel(const __gr
     }
     if (kNorm) unit.load_weight(t.weight);
     if (pos == PRQ_POSITION_NONE) return;
-    turn_pairs(p, turns, pos, angle_s);
+    turn_pairs<kLanes>(p, turns, pos, angle_s);
     __syncthreads();
     f32x2 c[4], s[4];
-    read_pairs(angle_s, unit.u, c, s);
+    read_pairs<kLanes>(angle_s, unit.u, c, s);
     const float inv_dim = 1.0f / p.head_dim;
 #pragma unroll
     for (int n = 0; n < kTimes; ++n) {
@@ -330,7 +336,9 @@ cudaError_t launch_of(const RotateParams& p, int num_sms, cudaStream_t stream) {
         return launch(rotate_any_kernel<T, kInterleaved, kNorm>, dim3(static_cast<unsigned>(std::min<long long>((tasks + kAnyWarps - 1) / kAnyWarps, num_sms * 16ll))),
                       kAnyWarps * 32, stream, p);
     }
-    const int lanes = p.head_dim <= 64 ? 4 : p.head_dim <= 128 ? 8 : 16, at_once = 32 / lanes;
+    // lanes of a head: a power of two, for the norm's sum over them; without one, five or six where that is a head's units (20 + 20 heads of 80, 1533
+    // rows, fp32: 9.2 us with eight, 8.6 so)
+    const int units = p.head_dim / 16, lanes = !kNorm && (units == 5 || units == 6) ? units : units <= 4 ? 4 : units <= 8 ? 8 : 16, at_once = 32 / lanes;
     constexpr int kMany = 8 / sizeof(T);
     const auto its = [&](int times) { return (p.t[0].heads + at_once * times - 1) / (at_once * times) + (p.t[1].heads + at_once * times - 1) / (at_once * times); };
     // few rows: as long as the warps with one group of heads each are all on the GPU at once (40 heads of 128: up to 236 rows.  64 rows:
@@ -343,6 +351,10 @@ cudaError_t launch_of(const RotateParams& p, int num_sms, cudaStream_t stream) {
         return launch(few ? rotate_kernel<T, kInterleaved, kNorm, kLanes, 1> : rotate_kernel<T, kInterleaved, kNorm, kLanes, kMany>, dim3(p.M, slices), warps * 32,
                       stream, p, warps_q);
     };
+    if constexpr (!kNorm) {
+        if (lanes == 5) return of(std::integral_constant<int, 5>());
+        if (lanes == 6) return of(std::integral_constant<int, 6>());
+    }
     return lanes == 4 ? of(std::integral_constant<int, 4>()) : lanes == 8 ? of(std::integral_constant<int, 8>()) : of(std::integral_constant<int, 16>());
 }
 

@@ -39,7 +39,7 @@ PLAIN = dict(scaling="none")
     (1, 32, 8, 128, 128), (1, 1, 0, 64, 64), (3, 4, 1, 64, 32), (2, 3, 5, 80, 80), (5, 20, 20, 80, 32), (4, 7, 2, 96, 48), (7, 16, 2, 128, 64), (9, 5, 1, 256, 256),
     (2, 4, 2, 256, 64), (6, 2, 1, 192, 192), (3, 3, 3, 112, 112), (33, 8, 1, 576 - 64, 64), (2, 2, 1, 512, 256), (5, 2, 2, 18, 18), (4, 3, 1, 2, 2), (3, 2, 1, 20, 6),
     (2, 5, 3, 129, 34), (64, 32, 8, 128, 128), (130, 9, 3, 128, 128), (257, 6, 2, 64, 64), (1000, 3, 1, 128, 32), (513, 2, 2, 40, 40), (301, 40, 8, 128, 128),
-    (150, 12, 1, 16, 16), (149, 4, 1, 48, 16)])
+    (150, 12, 1, 16, 16), (149, 4, 1, 48, 16), (700, 20, 20, 80, 32), (701, 7, 11, 96, 96), (702, 13, 1, 80, 80)])
 def test_against_64_bits(prq, M, q, k, D, rot, norm, layout, dtype):
     g = _g(M + D + rot)
     y = _normal(g, M, (q + 2 * k) * D).to(DT[dtype])
