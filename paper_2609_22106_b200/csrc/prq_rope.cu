@@ -260,7 +260,7 @@ __device__ __forceinline__ void read_pairs(const Angles<kLanes>& angle, int u, f
 // (kTimes = 4 for bf16, 2 for fp32) and 24 warps per SM.  The angles, a pair a thread, are worked out beside the loads.  (Rows that came
 // through a ring in shared memory by bulk copies, CTAs going from row to row, took longer: one barrier per row holds all warps.)  8192
 // rows of 40 heads of 128, bf16: 26.4 us, 6.35 TB/s; 4096 rows with the norm: 16.7 us, 5.0 TB/s, its instructions count there.  For few rows
-// the chain position -> angle -> result is what takes the time: one row 1.85 us, as long as an empty launch behind another.
+// the chain position -> angle -> result is what takes the time: one row 1.8 us, as long as an empty launch behind another.
 template <class T, bool kInterleaved, bool kNorm, int kLanes, int kTimes>
 __global__ void __launch_bounds__(kRotateWarps * 32, 3) rotate_kernel(const __grid_constant__ RotateParams p, int warps_q) {
     constexpr int kHeads = 32 / kLanes;
