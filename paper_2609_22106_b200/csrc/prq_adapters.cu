@@ -913,7 +913,7 @@ __global__ void __launch_bounds__(kHighThreads, 1) adapters_high_y_kernel(const 
     unsigned count = 0;            // tiles that were multiplied: accumulator and phase
     bool ok = true;
 #pragma unroll 1
-    while (at_tile < stop_tile) {
+    while (ok && at_tile < stop_tile) {
         // ---- the tiles of one part of one item
         const int nth = static_cast<int>(at_tile / tiles_per_item);
         int in_item = static_cast<int>(at_tile - static_cast<long long>(nth) * tiles_per_item);
@@ -1104,10 +1104,20 @@ __global__ void __launch_bounds__(kHighThreads, 1) adapters_high_y_kernel(const 
             __syncthreads();
             tc_fence_after_sync();
             if (tile + 1 < tiles && threadIdx.x == 0) multiply(tile + 1);
-            ok = ok && mbar_wait(smem_u32(&done[(count + tile) & 1]), (count + tile) >> 1 & 1, &abort_s);
+            // A warp takes the tile out as a whole or not at all.  Whether a wait ran out is the CTA's answer at the barrier behind the tile: nothing
+            // is multiplied, asked for or taken out after one did.
+            const unsigned number = count + tile;
+            const bool gives_up = p.wait_limit < 0 && threadIdx.x == 0 && static_cast<long long>(number) + 1 >= -p.wait_limit;
+            const bool there = __all_sync(0xffffffffu, !gives_up && mbar_wait(smem_u32(&done[number & 1]), number >> 1 & 1, &abort_s,
+                                                                              p.wait_limit < 0 ? kWaitLimitCycles : p.wait_limit));
             tc_fence_after_sync();
-            if (ok) take(tile);
-            __syncthreads();             // (the tile's places are free)
+            if (there) take(tile);
+            ok = __syncthreads_and(there);   // (the tile's places are free)
+            if (!ok) {
+                // products that are still on their way read shared memory and write tensor memory
+                for (unsigned i = number; i < count + min(tiles, tile + 2); ++i) mbar_wait_after_abort(smem_u32(&done[i & 1]), i >> 1 & 1);
+                break;
+            }
             ask_b(tile + 2);
             ask_base(tile + 2);
         }
@@ -1117,7 +1127,7 @@ __global__ void __launch_bounds__(kHighThreads, 1) adapters_high_y_kernel(const 
         __syncthreads();
         tc_fence_after_sync();
     }
-    if (!ok && lane == 0) atomicExch(p.status, PRQ_ERR_TIMEOUT);
+    if (!ok && threadIdx.x == 0) atomicExch(p.status, PRQ_ERR_TIMEOUT);
     tc_fence_before_sync();
     __syncthreads();
     if (warp == 0) tmem_dealloc(tmem, kTmemCols);

@@ -495,6 +495,7 @@ prq_status current_device_ready(int* num_sms, int** status) {
     return st;
 }
 void count_launches(int n) { g_launches.fetch_add(n); }
+int developer_switch(const char* name, int dflt) { return env_int(name, dflt); }
 }  // namespace prq
 
 extern "C" {

@@ -127,6 +127,9 @@ prq_status prq_linear_adapters(const prq_adapters* a, const int32_t* row_adapter
     p.ldbase = ldbase;
     p.ldy = ldy;
     p.M = M;
+    // developer switch: lets a test watch a wait run out
+    const int limit = developer_switch("PRQ_WAIT_LIMIT_CYCLES", 0);
+    p.wait_limit = limit ? limit : kDefaultWaitLimitCycles;
     int launches = 0;
     const cudaError_t e = launch_adapters(p, y_dtype == PRQ_BF16, sms, static_cast<cudaStream_t>(stream), &launches);
     count_launches(launches);

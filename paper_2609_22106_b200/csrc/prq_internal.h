@@ -156,9 +156,10 @@ struct SfLayouts { int n, n_experts, group_bytes; SfLayout l[5]; };   // group_b
 cudaError_t launch_sf_layout(const uint8_t* scales, int N, int K, int k_tail, const SfLayouts& t, int sm_count, cudaStream_t stream);
 
 // For entry points that take no handle (prq_api.cu): whether the current device can run the kernels, with its SM count and status word; and the
-// library's count of its launches.
+// library's count of its launches; and a developer switch (its default but in processes with PRQ_DEV=1).
 prq_status current_device_ready(int* num_sms, int** status);
 void count_launches(int n);
+int developer_switch(const char* name, int dflt);
 
 }  // namespace prq
 

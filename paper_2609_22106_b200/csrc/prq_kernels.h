@@ -248,6 +248,7 @@ struct AdapterParams {
     int h_clusters, y_items;     // clusters, and groups of CTAs, per window: each has every so many-th item
     int part_end[kMaxBatch];     // column behind each part
     int unit_end[kMaxBatch];     // pieces of columns up to the end of each part, as the launch cuts them
+    long long wait_limit;        // SM clock cycles after which a wait for the tensor core gives up; -n: a CTA's nth such wait counts as run out
 };
 size_t adapters_workspace_bytes(int M, int n_slots, int n_parts, int max_rank, bool any_fewer);   // any_fewer: enough for up to M rows
 cudaError_t launch_adapters(const AdapterParams& p, bool bf16, int num_sms, cudaStream_t stream, int* launches);

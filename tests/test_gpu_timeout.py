@@ -62,3 +62,36 @@ def test_fixup_wait_runs_out_and_the_next_call_is_correct(prq, oracle, monkeypat
     got = y_again[torch.from_numpy(rows).cuda()].cpu().numpy().astype(np.float64)
     assert np.abs(got - y_ref).max() <= 2e-3 * (np.abs(y_ref).max() + 1)
     w.free()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("R,parts,tile", [(64, [9728], 1), (64, [9728], 2), (64, [5120, 4605], 3), (128, [5120], 1), (128, [5120], 4), (120, [4608, 515], 2)])
+def test_adapters_whose_wait_for_the_tensor_core_runs_out(prq, monkeypatch, R, parts, tile, dtype):
+    """The kernel for adapters of high ranks.  Its waits are for its own products, which always end: a developer switch makes one thread of every
+    CTA take the wait for its nth tile as run out, while the products of that tile and of the next one may be on their way.  The whole
+    CTA leaves; what it had stored by then is right, the rest of y is untouched, and the next call is right."""
+    M, K, S, N = 4096, 64, 3, sum(parts)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(R + tile)
+    normal = lambda *shape: torch.randn(*shape, generator=g, device="cuda")
+    x = normal(M, K).to(torch.bfloat16)
+    A, B = (normal(S, len(parts), R, K) * 0.05).to(torch.bfloat16), (normal(S, N, R) * 0.2).to(torch.bfloat16)
+    base, good, out = (t[:, :N] for t in (normal(M, (N + 7) // 8 * 8).to(dtype), *torch.full((2, M, (N + 7) // 8 * 8), float("nan"), dtype=dtype, device="cuda")))
+    rows = torch.randint(0, S, (M,), generator=g, device="cuda", dtype=torch.int32)
+    pool = prq.Adapters(A, B, parts)
+    ws = prq.adapters_workspace(pool, M)
+    prq.linear_adapters(pool, x, rows, base, out=good, workspace=ws)
+    assert prq.last_device_status() == 0
+    monkeypatch.setenv("PRQ_WAIT_LIMIT_CYCLES", str(-tile))
+    t0 = time.time()
+    prq.linear_adapters(pool, x, rows, base, out=out, workspace=ws)
+    status = prq.last_device_status()                    # synchronises
+    assert time.time() - t0 < 1.0
+    monkeypatch.delenv("PRQ_WAIT_LIMIT_CYCLES")
+    assert status == PRQ_ERR_TIMEOUT and prq.last_device_status() == 0
+    stored = ~torch.isnan(out)
+    assert torch.equal(out[stored], good[stored]) and not stored.all()
+    if tile > 1:
+        assert stored.any()
+    prq.linear_adapters(pool, x, rows, base, out=out, workspace=ws)
+    assert prq.last_device_status() == 0 and torch.equal(out, good)
