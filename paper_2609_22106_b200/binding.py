@@ -554,8 +554,9 @@ def _load_torch():
     global _torch, _f32, _bf16, _i32, _current_device
     import torch
 
-    _torch, _f32, _bf16, _i32 = torch, torch.float32, torch.bfloat16, torch.int32
+    _f32, _bf16, _i32 = torch.float32, torch.bfloat16, torch.int32
     _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _torch = torch   # last: a thread that finds it set reads the others
 
 
 ADAPTER_MAX_RANK = 128

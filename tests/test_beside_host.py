@@ -1,6 +1,8 @@
 """Adapters and position rotation, what needs no GPU: refusals, frequencies, the fold, what a call launches."""
 import ctypes
+import importlib.util
 import math
+import sys
 
 import numpy as np
 import pytest
@@ -165,3 +167,27 @@ def test_heads_refused(fake, status, q, call):  # noqa: F811
 def test_more_heads_than_a_row_can_have(fake):  # noqa: F811
     assert _rotate(fake, _heads(fake, heads=65536, ldx=1 << 23, ldout=1 << 23)) == (0, 1)
     assert _rotate(fake, _heads(fake, heads=65537, ldx=1 << 23, ldout=1 << 23)) == (1, 0)
+
+
+def test_a_thread_that_finds_torch_loaded_finds_all_of_its_names(prq):
+    """Two threads' first calls may meet: at no line of the load is torch set and another name not."""
+    pytest.importorskip("torch")
+    spec = importlib.util.spec_from_file_location("prq_binding_loaded_anew", prq.__file__)
+    anew = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(anew)
+    bad, lines = [], []
+
+    def step(frame, event, arg):
+        if frame.f_code is anew._load_torch.__code__:
+            lines.append(frame.f_lineno)
+            if anew._torch is not None and None in (anew._f32, anew._bf16, anew._i32, anew._current_device):
+                bad.append(frame.f_lineno)
+            return step
+
+    before = sys.gettrace()
+    sys.settrace(step)
+    try:
+        anew._load_torch()
+    finally:
+        sys.settrace(before)
+    assert anew._torch is not None and len(set(lines)) > 3 and not bad
