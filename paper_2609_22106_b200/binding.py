@@ -740,4 +740,5 @@ def rotate_heads(rope: Rope, positions, q, k=None, out=None, stream=None):
 
 def norm_rotate_heads(rope: Rope, positions, q, k=None, q_weight=None, k_weight=None, eps: float = 1e-6, out=None, stream=None):
     """The RMS norm of every head (weights: fp32 (head_dim,) or None), then rotate_heads, in one pass."""
+    _require(eps is not None, "prq_norm_rotate_heads")   # (to _rotate None means: no norm)
     return _rotate(rope, positions, q, k, q_weight, k_weight, eps, out, stream, "prq_norm_rotate_heads")

@@ -191,3 +191,37 @@ def test_a_thread_that_finds_torch_loaded_finds_all_of_its_names(prq):
     finally:
         sys.settrace(before)
     assert anew._torch is not None and len(set(lines)) > 3 and not bad
+
+
+class _Tensor:
+    """What the binding asks of a CUDA tensor, over host bytes (device memory to the stand-in)."""
+
+    def __init__(self, torch, shape, stride, dtype, device=0):
+        self.shape, self._stride, self.dtype, self._device, self._bytes = torch.Size(shape), tuple(stride), dtype, device, _aligned(1 << 16)
+
+    stride = lambda self: self._stride
+    dim = lambda self: len(self.shape)
+    get_device = lambda self: self._device
+    data_ptr = lambda self: self._bytes.ctypes.data
+    is_contiguous = lambda self: True
+
+
+@pytest.fixture
+def tensors(fake, monkeypatch):  # noqa: F811
+    """The binding over the stand-in with such tensors on its device 0, and a stream to pass."""
+    torch = pytest.importorskip("torch")
+    fake._load_torch()
+    monkeypatch.setattr(fake, "_current_device", lambda: 0)
+    return torch, lambda *a, **o: _Tensor(torch, *a, **o), type("Stream", (), {"cuda_stream": 0})
+
+
+def test_a_norm_without_its_eps_is_refused(fake, tensors):  # noqa: F811
+    """... and not taken for a rotation without a norm."""
+    torch, tensor, stream = tensors
+    rope, positions, q = fake.Rope(64), tensor((3,), (1,), torch.int32), tensor((3, 2, 64), (128, 64, 1), torch.bfloat16)
+    n = fake.kernel_launch_count()
+    for eps in (None, 0.0, -1.0, math.nan):
+        with pytest.raises(fake.PrqError):
+            fake.norm_rotate_heads(rope, positions, q, eps=eps, stream=stream)
+    assert fake.kernel_launch_count() == n
+    assert fake.norm_rotate_heads(rope, positions, q, eps=1e-5, stream=stream) is q and fake.kernel_launch_count() == n + 1
