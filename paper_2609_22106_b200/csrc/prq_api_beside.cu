@@ -82,7 +82,7 @@ prq_status rotate(const prq_rope* r, const int32_t* positions, int M, const prq_
     p.factor = static_cast<float>(r->attention_factor);
     std::memcpy(p.turns, r->turns, sizeof(p.turns));
     const cudaError_t e = launch_rotate_heads(p, r->layout == PRQ_ROPE_INTERLEAVED, norm, dtype == PRQ_BF16, sms, static_cast<cudaStream_t>(stream));
-    count_launches(1);
+    count_launches(e == cudaSuccess);
     return e == cudaSuccess ? PRQ_OK : PRQ_ERR_CUDA;
 }
 

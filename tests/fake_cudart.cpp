@@ -37,6 +37,7 @@ int g_last_grid = 0, g_last_cluster = 0;
 unsigned g_fill = 1;
 int g_mallocs, g_frees;   // calls; of null pointers not counted
 int g_fail_in = 0;        // the allocation that fails, counted from the next one (0: none)
+int g_fail_launch_in = 0; // the launch that fails, the same way
 
 void run(Stream* s) {
     for (auto& w : s->work) w();
@@ -69,6 +70,7 @@ cudaError_t copy(void* dst, const void* src, size_t n, cudaMemcpyKind kind, Stre
 }
 cudaError_t launch(const void* func, dim3 grid, size_t dynamic_smem) {
     std::lock_guard<std::mutex> lock(g_mu);
+    if (g_fail_launch_in > 0 && --g_fail_launch_in == 0) return t_last = cudaErrorLaunchOutOfResources;
     auto it = g_dynamic_smem.find({t_device, func});
     if (dynamic_smem > static_cast<size_t>(it == g_dynamic_smem.end() ? 48 * 1024 : it->second)) return t_last = cudaErrorInvalidValue;
     ++g_launches[t_device];
@@ -93,6 +95,7 @@ int fake_last_cluster() { return g_last_cluster; }       // CTAs per cluster
 int fake_mallocs() { return g_mallocs; }
 int fake_frees() { return g_frees; }
 void fake_fail_malloc(int nth) { g_fail_in = nth; }
+void fake_fail_launch(int nth) { g_fail_launch_in = nth; }
 int fake_pending() {   // operations that no wait has covered yet
     std::lock_guard<std::mutex> lock(g_mu);
     size_t n = g_legacy.work.size();

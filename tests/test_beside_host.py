@@ -225,3 +225,17 @@ def test_a_norm_without_its_eps_is_refused(fake, tensors):  # noqa: F811
             fake.norm_rotate_heads(rope, positions, q, eps=eps, stream=stream)
     assert fake.kernel_launch_count() == n
     assert fake.norm_rotate_heads(rope, positions, q, eps=1e-5, stream=stream) is q and fake.kernel_launch_count() == n + 1
+
+
+def test_a_launch_that_fails_is_not_counted(fake):  # noqa: F811
+    L, h = fake.lib(), _heads(fake)
+    for eps in (None, 1e-6):
+        L.fake_fail_launch(1)
+        assert _rotate(fake, h, h, eps=eps) == (4, 0) and _rotate(fake, h, h, eps=eps) == (0, 1)
+    for M, nth in ((3, 1), (513, 1), (513, 2)):           # one launch, the first and the second one of two
+        before = fake.kernel_launch_count()
+        L.fake_fail_launch(nth)
+        pool, some, ws = _pool(fake), _aligned(16).ctypes.data, _aligned(1 << 20).ctypes.data
+        call = lambda: L.prq_linear_adapters(ctypes.addressof(pool), some, some, M, 64, some, 48, some, 48, 0, ws, 1 << 20, None)
+        assert call() == 4 and fake.kernel_launch_count() == before + nth - 1
+        assert call() == 0
