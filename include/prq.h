@@ -494,7 +494,7 @@ typedef struct prq_rope_opts {
     double beta_slow;          /* YARN [1]                                                     */
     double low_factor;         /* WAVELENGTH [1]                                               */
     double high_factor;        /* WAVELENGTH, > low_factor [4]                                 */
-    double attention_factor;   /* what rotated elements are multiplied by [YARN as above, otherwise 1] */
+    double attention_factor;   /* what rotated elements are multiplied by, within fp32's range [YARN as above, otherwise 1] */
 } prq_rope_opts;
 
 /* Host only: a handle belongs to no device, is immutable, and may be used by several threads and streams. */

@@ -151,7 +151,8 @@ prq_status prq_rope_create(const prq_rope_opts* opts, prq_rope** out) {
     if (o.head_dim < 2 || o.head_dim > 512 || o.rot_dim < 2 || o.rot_dim % 2 || o.rot_dim > o.head_dim || o.rot_dim > 2 * kMaxPairs) return PRQ_ERR_INVALID_ARG;
     if (o.layout != PRQ_ROPE_HALF && o.layout != PRQ_ROPE_INTERLEAVED) return PRQ_ERR_INVALID_ARG;
     if (!(o.base > 1.0) || !std::isfinite(o.base) || !(o.factor >= 1.0) || !std::isfinite(o.factor)) return PRQ_ERR_INVALID_ARG;
-    if (!(o.attention_factor >= 0.0) || !std::isfinite(o.attention_factor)) return PRQ_ERR_INVALID_ARG;
+    const float attention_factor = static_cast<float>(o.attention_factor);   // (what a kernel multiplies by)
+    if (!(o.attention_factor >= 0.0) || !std::isfinite(attention_factor) || (o.attention_factor > 0.0 && attention_factor == 0.0f)) return PRQ_ERR_INVALID_ARG;
 
     long double base = o.base, low = 0.0l, high = 0.0l, attention = 1.0l;
     const long double two_pi = 2.0l * acosl(-1.0l);

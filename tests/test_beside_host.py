@@ -239,3 +239,12 @@ def test_a_launch_that_fails_is_not_counted(fake):  # noqa: F811
         call = lambda: L.prq_linear_adapters(ctypes.addressof(pool), some, some, M, 64, some, 48, some, 48, 0, ws, 1 << 20, None)
         assert call() == 4 and fake.kernel_launch_count() == before + nth - 1
         assert call() == 0
+
+
+def test_a_factor_that_is_no_fp32_number_is_refused(prq):
+    """Kernels multiply by it in fp32: one beyond that range would turn every element into infinities or zeros."""
+    for bad in (1e39, 1.7e308, 1e-46, 5e-324):
+        with pytest.raises(prq.PrqError):
+            prq.Rope(64, attention_factor=bad)
+    for good in (3.4e38, 1e-45, 0.5):
+        assert prq.Rope(64, attention_factor=good).frequencies()[1] == good
