@@ -559,6 +559,7 @@ def _load_torch():
     _torch = torch   # last: a thread that finds it set reads the others
 
 
+_INT_MAX = 2 ** 31 - 1
 ADAPTER_MAX_RANK = 128
 ADAPTER_FEW_ROWS, ADAPTER_FEW_RANKS = 512, 64   # up to that many rows, and ranks of all parts in whole 16s, a call needs no workspace
 
@@ -624,6 +625,8 @@ def linear_adapters(adapters: Adapters, x, row_adapter, base, out=None, workspac
     if M == 1:   # a single row has no stride
         ldx, ldbase = K, (N + 7) // 8 * 8
         ldout = ldbase
+    elif max(ldx, ldbase, ldout) > _INT_MAX:   # (ctypes would pass what is left of it in 32 bits)
+        _require(False, where)
     if workspace is None:
         if M > adapters._free_rows:
             if stream is None:

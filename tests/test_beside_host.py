@@ -248,3 +248,22 @@ def test_a_factor_that_is_no_fp32_number_is_refused(prq):
             prq.Rope(64, attention_factor=bad)
     for good in (3.4e38, 1e-45, 0.5):
         assert prq.Rope(64, attention_factor=good).frequencies()[1] == good
+
+
+def test_row_strides_beyond_an_int_are_refused(fake, tensors):  # noqa: F811
+    """... and not cut to 32 bits on their way to the C call, which would read and write other rows."""
+    torch, tensor, stream = tensors
+    K, N, far = 64, 48, 2 ** 32 + 64
+    pool = fake.Adapters.__new__(fake.Adapters)
+    pool._pool = _pool(fake, K=K, parts=(N,))
+    pool.K, pool.N, pool.device, pool._free_rows, pool._p = K, N, 0, 512, ctypes.addressof(pool._pool)
+    rows = lambda M: tensor((M,), (1,), torch.int32)
+    matrix = lambda M, n, ld, dtype=torch.bfloat16: tensor((M, n), (ld, 1), dtype)
+    n = fake.kernel_launch_count()
+    for ldx, ldb, ldy in ((far, 48, 48), (64, far, far), (64, far, 48), (64, 48, far)):
+        with pytest.raises(fake.PrqError):
+            fake.linear_adapters(pool, matrix(2, K, ldx), rows(2), matrix(2, N, ldb), out=matrix(2, N, ldy), stream=stream)
+    assert fake.kernel_launch_count() == n
+    for M, ld in ((2, 2 ** 31 - 8), (1, far)):           # the largest one; a single row has none
+        fake.linear_adapters(pool, matrix(M, K, ld), rows(M), matrix(M, N, ld), out=matrix(M, N, ld), stream=stream)
+    assert fake.kernel_launch_count() == n + 2
