@@ -561,7 +561,7 @@ def _load_torch():
 
 _INT_MAX = 2 ** 31 - 1
 ADAPTER_MAX_RANK = 128
-ADAPTER_FEW_ROWS, ADAPTER_FEW_RANKS = 512, 64   # up to that many rows, and ranks of all parts in whole 16s, a call needs no workspace
+ADAPTER_FEW_ROWS = 512   # calls on up to that many rows do not ask the library each time whether they need a workspace
 
 
 class AdapterPool(ctypes.Structure):
@@ -588,9 +588,9 @@ class Adapters:
         _require(all(t is None or t.get_device() == A.get_device() for t in (B, scale, ranks)) and A.is_cuda, where)
         self.A, self.B, self.scale, self.ranks, self.parts, self.N, self.K = A, B, scale, ranks, parts, sum(parts), K
         self.device = A.get_device()
-        self._free_rows = ADAPTER_FEW_ROWS if P * ((R + 15) // 16 * 16) <= ADAPTER_FEW_RANKS else 0
         self._pool = AdapterPool(ctypes.sizeof(AdapterPool), S, R, K, P, (ctypes.c_int * 4)(*parts), _dptr(A), _dptr(B), _dptr(scale), _dptr(ranks))
         self._p = ctypes.addressof(self._pool)
+        self._free_rows = 0 if lib().prq_adapters_workspace_bytes(self._p, ADAPTER_FEW_ROWS) else ADAPTER_FEW_ROWS   # (the answer is for up to so many)
 
 
 def adapters_workspace(adapters: Adapters, M: int):

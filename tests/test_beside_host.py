@@ -267,3 +267,19 @@ def test_row_strides_beyond_an_int_are_refused(fake, tensors):  # noqa: F811
     for M, ld in ((2, 2 ** 31 - 8), (1, far)):           # the largest one; a single row has none
         fake.linear_adapters(pool, matrix(M, K, ld), rows(M), matrix(M, N, ld), out=matrix(M, N, ld), stream=stream)
     assert fake.kernel_launch_count() == n + 2
+
+
+@pytest.mark.parametrize("answer", [None, 64])
+def test_whether_a_call_needs_a_workspace_is_what_the_library_says(fake, tensors, monkeypatch, answer):  # noqa: F811
+    """None: as it is; 64: a library that wants one of every call."""
+    torch, tensor, _ = tensors
+    ask = fake.lib().prq_adapters_workspace_bytes
+    if answer:
+        monkeypatch.setattr(fake.lib(), "prq_adapters_workspace_bytes", lambda p, M: answer)
+    for S, parts, R in ((4, [64], 8), (4, [64, 32], 16), (4, [32, 32, 32], 16), (4, [32, 32, 32, 32], 24), (2, [64], 64), (2, [64], 72), (2, [64, 64], 40), (600, [64], 128)):
+        A, B = tensor((S, len(parts), R, 64), (1, 1, 1, 1), torch.bfloat16), tensor((S, sum(parts), R), (1, 1, 1), torch.bfloat16)
+        A.is_cuda = True
+        pool = fake.Adapters(A, B, parts)
+        assert all((answer or ask(pool._p, M)) == 0 for M in range(1, pool._free_rows + 1))
+        if not answer and len(parts) * R <= 64 and R % 16 == 0:
+            assert pool._free_rows == 512
