@@ -448,7 +448,9 @@ size_t prq_adapters_workspace_bytes(const prq_adapters *a, int M);
  * The kernels read row_adapter, ranks, scale, A and B when they run: a captured call follows what a program writes there before it is
  * replayed.  None of them may change while the call runs.  One launch where no workspace is needed, two otherwise.  A wait in a kernel that
  * ran out leaves PRQ_ERR_TIMEOUT in the device status (prq_last_device_status), and y incomplete.
- * A value that is not finite in x, or in an adapter, reaches the rows of that row's, of that adapter's requests only.
+ * A value that is not finite in x, or in an adapter, reaches the rows of that row's, of that adapter's requests only.  An infinity in x or A
+ * comes out with the sign of its product; an infinity in B as an infinity or NaN (its two products with the two terms of the low-rank
+ * product may cancel), in its column alone.
  * Errors: INVALID_ARG (M of 2^23 rows and more among it), ALIGNMENT, WORKSPACE, UNSUPPORTED_ARCH, CUDA.  M == 0 is a no-op. */
 prq_status prq_linear_adapters(const prq_adapters *a, const int32_t *row_adapter, const void *x, int M, int ldx, const void *base,
                                int ldbase, void *y, int ldy, prq_dtype y_dtype, void *workspace, size_t workspace_bytes,

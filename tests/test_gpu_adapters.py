@@ -232,3 +232,24 @@ def test_an_attention_blocks_projections_as_they_are_used(prq, oracle):
         assert ((t.double() - want).abs() <= bound).all()
     assert torch.equal(y[:, parts[0] + parts[1]:], before[:, parts[0] + parts[1]:])      # v is left alone
     assert prq.last_device_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,R,parts", [(6, 128, 16, [72]), (90, 96, 24, [40, 33]), (700, 128, 16, [72]), (700, 128, 48, [72]), (700, 64, 128, [72, 19]), (8192, 64, 64, [5120])])
+def test_an_adapter_that_is_not_finite_marks_its_own_rows(prq, M, K, R, parts, dtype):
+    """An infinity in A: every column of its part, in every row of the adapter; in B: its column.  All other results are as ever."""
+    S, N = 4, sum(parts)
+    g, x, A, B, base = _inputs(M + R, M, K, parts, R, S, dtype)
+    rows = _rows("mix", M, S, g)
+    rows[:4] = torch.arange(4, dtype=torch.int32, device="cuda")
+    A[1, -1, R - 1, 3] = float("inf")
+    B[2, 7, 1], B[2, N - 1, R - 1] = float("inf"), -float("inf")
+    out = torch.zeros(M, base.stride(0), dtype=base.dtype, device="cuda")[:, :N]
+    got = prq.linear_adapters(prq.Adapters(A, B, parts), x, rows, base, out=out)
+    bad = torch.zeros(M, N, dtype=torch.bool, device="cuda")
+    bad[rows == 1, N - parts[-1]:] = True
+    bad[(rows == 2).nonzero(), torch.tensor([[7, N - 1]], device="cuda")] = True
+    assert torch.equal(~torch.isfinite(got), bad)
+    A[1, -1, R - 1, 3] = B[2, 7, 1] = B[2, N - 1, R - 1] = 0
+    want, bound = beside_ref.adapters_of_many(x, A, B, parts, rows, base)
+    assert ((got.double() - want).abs() <= bound)[~bad].all()
