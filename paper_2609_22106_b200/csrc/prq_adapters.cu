@@ -811,33 +811,27 @@ __global__ void __launch_bounds__(kManyThreads, kSteps16 == 1 ? 3 : 2) adapters_
 // after another.  A tile of base comes into shared memory while the one before is done; the tensor core multiplies the item's h, which stays in
 // shared memory as 128 x 2 rank (hi, then lo against the same B), with the next tile's B into one of two accumulators in tensor memory
 // while the threads take this tile out of the other one, add base in its place, and store rows from there.
-// Operands lie in the tensor core's swizzled layout of 32, 64 or 128 bytes of K per row (a rank of 128 takes two such blocks): the pieces of a
+// Operands lie in the tensor core's swizzled layout of 128 bytes of K per row (ranks above 64 take two such blocks): the pieces of a
 // row, which neighbouring threads copy, stay within 128 bytes.  (Without swizzle each goes to a line of shared memory of its own, and
 // the copies of one tile of B took 2500 cycles instead of 300.)  Rows of base: piece i of row r (16 bytes) at
 // i ^ (r & 7), so that eight threads with a row each meet no bank twice.
 // Bound by shared memory, which a tile passes five times (base and B in, operands, base again, and out): 4096 rows of gate / up in place, rank
 // 64, 87 us for 319 MB, 3.7 TB/s; with fragments from shared memory (mma.sync) 110.
 constexpr int kHighThreads = 512, kHighWarps = kHighThreads / 32;
-struct HighShared { int k_bytes, blocks, h, base, b, total; };   // bytes of K per row, blocks of them; bytes of h, a tile of base, of B, and in all, with two of each tile
+constexpr int kKBytes = 128;      // of K per row of an operand's block
+struct HighShared { int blocks, h, base, b, total; };   // blocks of K; bytes of h, a tile of base, of B, and in all, with two of each tile
 __host__ __device__ inline HighShared high_shared(int pad_rank, int row_bytes, int cols) {
     HighShared t;
-    t.k_bytes = pad_rank <= 16 ? 32 : pad_rank <= 32 ? 64 : 128;
     t.blocks = pad_rank <= 64 ? 1 : 2;
-    t.h = 2 * t.blocks * kManyRows * t.k_bytes;
+    t.h = 2 * t.blocks * kManyRows * kKBytes;
     t.base = kManyRows * row_bytes;
-    t.b = t.blocks * cols * t.k_bytes;
+    t.b = t.blocks * cols * kKBytes;
     t.total = 1024 + t.h + 2 * (t.base + t.b);   // (the first kilobyte: alignment)
     return t;
 }
 // Where 16-byte piece c of row r of an operand with `rows` rows lies.
-__device__ __forceinline__ uint32_t operand_at(int r, int c, int rows, int k_bytes) {
-    if (k_bytes == 32) return r * 32 + 16 * (c ^ (r >> 2 & 1));
-    if (k_bytes == 64) return r * 64 + 16 * (c ^ (r >> 1 & 3));
-    return (c >> 3) * rows * 128 + r * 128 + 16 * ((c ^ r) & 7);
-}
-__device__ __forceinline__ uint64_t operand_desc(uint32_t at, int k_bytes) {
-    return make_smem_desc(at, 16, 8 * k_bytes, k_bytes == 32 ? kSwizzle32B : k_bytes == 64 ? kSwizzle64B : kSwizzle128B);
-}
+__device__ __forceinline__ uint32_t operand_at(int r, int c, int rows) { return (c >> 3) * rows * kKBytes + r * kKBytes + 16 * ((c ^ r) & 7); }
+__device__ __forceinline__ uint64_t operand_desc(uint32_t at) { return make_smem_desc(at, 16, 8 * kKBytes, kSwizzle128B); }
 // The nth item of all windows that has something to do; -1 and the number of them in `all` if there are not so many.
 __device__ __forceinline__ int nth_item(const int* counts, const AdapterItems& t, int nth, int* shared, int* all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -965,7 +959,7 @@ __global__ void __launch_bounds__(kHighThreads, 1) adapters_high_y_kernel(const 
         const int b_rows_on = kHighThreads / b_pieces, b_pieces_on = kHighThreads - b_rows_on * b_pieces;
         const bool b_regular = b_pieces_on == 0 && (rank & 7) == 0;
         const uint16_t* b_from = B + static_cast<long long>(b_row) * p.max_rank + 8 * b_piece;
-        const uint32_t b_to = smem_u32(b_tiles) + operand_at(b_row, b_piece, kCols, lay.k_bytes);
+        const uint32_t b_to = smem_u32(b_tiles) + operand_at(b_row, b_piece, kCols);
         const long long b_step = static_cast<long long>(b_rows_on) * p.max_rank, b_tile_step = static_cast<long long>(kCols) * p.max_rank;
         auto ask_b = [&](int tile) {
             if (tile < tiles) {
@@ -976,12 +970,12 @@ __global__ void __launch_bounds__(kHighThreads, 1) adapters_high_y_kernel(const 
                     for (int row = b_row; row < here; row += b_rows_on) {
                         copy16(to, from);
                         from += b_step;
-                        to += b_rows_on * (b_piece >= 8 ? 128 : lay.k_bytes);
+                        to += b_rows_on * kKBytes;
                     }
                 } else {
                     for (int row = b_row, c = b_piece; row < here;) {
                         const uint16_t* from = B + static_cast<long long>(n + row) * p.max_rank + 8 * c;
-                        const uint32_t off = (tile & 1) * lay.b + operand_at(row, c, kCols, lay.k_bytes);
+                        const uint32_t off = (tile & 1) * lay.b + operand_at(row, c, kCols);
                         if (c < b_whole) {
                             copy16(smem_u32(b_tiles) + off, from);
                         } else {   // the piece that the rank ends in
@@ -1013,23 +1007,23 @@ __global__ void __launch_bounds__(kHighThreads, 1) adapters_high_y_kernel(const 
         for (int m = warp; m < rows; m += kHighWarps) {
             const uint2* from = reinterpret_cast<const uint2*>(ws.h + static_cast<long long>(row_s[m]) * (ranks / 4) + part * (pad_rank / 4));
             for (int c = lane; c < pad_rank / 2; c += 32)
-                copy8(smem_u32(h_tile) + (c & 1) * (lay.h / 2) + operand_at(m, c >> 2, kManyRows, lay.k_bytes) + 8 * (c >> 1 & 1), from + c);
+                copy8(smem_u32(h_tile) + (c & 1) * (lay.h / 2) + operand_at(m, c >> 2, kManyRows) + 8 * (c >> 1 & 1), from + c);
         }
         ask_b(0);
         ask_base(0);
         ask_b(1);
         ask_base(1);
 
-        const uint64_t h_desc = operand_desc(smem_u32(h_tile), lay.k_bytes);
+        const uint64_t h_desc = operand_desc(smem_u32(h_tile));
         const int k_steps = (rank + 15) / 16;
         auto multiply = [&](int tile) {   // one thread
             const unsigned number = count + tile;
-            const uint64_t b_desc = operand_desc(smem_u32(b_tiles) + (tile & 1) * lay.b, lay.k_bytes);
+            const uint64_t b_desc = operand_desc(smem_u32(b_tiles) + (tile & 1) * lay.b);
             for (int term = 0; term < 2; ++term)
                 for (int k = 0; k < k_steps; ++k) {
                     // (16 of K: 32 bytes on; a block of 64 of K: the next one)
-                    const uint64_t h_at = h_desc + ((term * (lay.h / 2) + (k >> 2) * kManyRows * 128 + (k & 3) * 32) >> 4);
-                    const uint64_t b_at = b_desc + (((k >> 2) * kCols * 128 + (k & 3) * 32) >> 4);
+                    const uint64_t h_at = h_desc + ((term * (lay.h / 2) + (k >> 2) * kManyRows * kKBytes + (k & 3) * 32) >> 4);
+                    const uint64_t b_at = b_desc + (((k >> 2) * kCols * kKBytes + (k & 3) * 32) >> 4);
                     tc_mma_bf16(tmem + (number & 1) * kCols, h_at, b_at, make_idesc_bf16(kCols), term | k);
                 }
             tc_commit(smem_u32(&done[number & 1]));

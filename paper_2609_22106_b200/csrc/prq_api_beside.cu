@@ -71,8 +71,8 @@ prq_status rotate(const prq_rope* r, const int32_t* positions, int M, const prq_
     if (heads == 0) return PRQ_OK;
     if (!positions) return PRQ_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(positions) % 4) return PRQ_ERR_ALIGNMENT;
-    int sms = 0;
-    const prq_status st = current_device_ready(&sms, &p.status);
+    int sms = 0, *status;   // (no wait of these kernels can run out)
+    const prq_status st = current_device_ready(&sms, &status);
     if (st != PRQ_OK) return st;
     p.positions = positions;
     p.M = M;

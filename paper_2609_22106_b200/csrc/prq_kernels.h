@@ -222,7 +222,6 @@ struct RotateParams {
     int M;
     int head_dim, rot_dim;
     float eps, factor;
-    int* status;                 // device status word
     uint64_t turns[kMaxPairs];   // fraction of a turn per position, in 2^-64
 };
 cudaError_t launch_rotate_heads(const RotateParams& p, bool interleaved, bool norm, bool bf16, int num_sms, cudaStream_t stream);

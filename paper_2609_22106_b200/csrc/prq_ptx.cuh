@@ -285,7 +285,7 @@ __device__ __forceinline__ void tmem_ld_wait() {
 // ---------------------------------------------------------------- descriptors
 // Shared-memory matrix descriptor (sm_100 format): start address and the two byte offsets in
 // 16-byte units, version 1 in bits [46,48), swizzle mode in bits [61,64).
-constexpr uint64_t kSwizzleNone = 0, kSwizzle128B = 2, kSwizzle64B = 4, kSwizzle32B = 6;
+constexpr uint64_t kSwizzleNone = 0, kSwizzle128B = 2;
 __host__ __device__ __forceinline__ uint64_t make_smem_desc(uint32_t smem_addr, uint32_t lbo_bytes,
                                                             uint32_t sbo_bytes, uint64_t swizzle) {
     return (uint64_t)((smem_addr & 0x3FFFF) >> 4) | ((uint64_t)(lbo_bytes >> 4) << 16) |
