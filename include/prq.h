@@ -413,7 +413,10 @@ prq_status prq_forward_host(const prq_weights *w, prq_act_mode mode, const uint1
  *   y[m, n] = base[m, n] + scale[a] * sum_{r < rank[a]} (sum_k x[m, k] A[a][p][r][k]) * B[a][n][r],    a = row_adapter[m],
  * p the part that column n lies in.  Parts are the layers of a stacked projection (q / k / v, gate / up): they read the same x, and
  * each has its own A.  One pool holds the adapters of all requests, a program writes an adapter's matrices into a free slot.
- * The sums are held in fp32; the low-rank product in between is kept to 16 bits or more of significand, y is rounded once.  */
+ * The sums are held in fp32; the low-rank product in between is kept to 16 bits or more of significand, also for an fp32 y; y is rounded once.
+ * For prq_linear and what else writes y to memory.  Two calls leave no room for an adapter: prq_linear_gated, which applies silu(gate) * up
+ * and quantises before anything is written (with adapters on gate / up take the plain stacked layer, and gate and quantise its sum; the
+ * down projection's adapters read that bf16 activation), and prq_linear_grouped, whose experts have no form here.  */
 #define PRQ_ADAPTER_MAX_RANK 128
 typedef struct prq_adapters {
     size_t struct_size;          /* sizeof(prq_adapters)                                                         */
@@ -482,7 +485,8 @@ typedef enum {
     PRQ_ROPE_WAVELENGTH = 4    /* from f_i to f_i / factor linearly in the turns t_i = original_positions f_i / 2 pi: f_i where
                                   t_i >= high_factor, f_i / factor where t_i <= low_factor                             */
 } prq_rope_scaling;
-/* Set struct_size = sizeof(prq_rope_opts).  Zero means the default in brackets; fields that a scaling does not use are not read. */
+/* Set struct_size = sizeof(prq_rope_opts).  Zero means the default in brackets.  base, factor and attention_factor must be valid with every
+ * scaling; of the fields behind factor a scaling reads those that name it. */
 typedef struct prq_rope_opts {
     size_t struct_size;
     int head_dim;              /* 2 .. 512                                                     */
@@ -528,7 +532,8 @@ prq_status prq_rotate_heads(const prq_rope *r, const int32_t *positions, int M, 
                             prq_stream_t stream);
 
 /* The same with the RMS norm of every head in front, in one pass over the data: z = x / sqrt(mean(x^2) + eps) * weight over the
- * whole head, in fp32, then the rotation of z.  eps > 0. */
+ * whole head, in fp32 (of a head whose squares pass fp32's range, elements of 1.8e19 and more, nothing but zeros is left), then the rotation
+ * of z.  eps > 0. */
 prq_status prq_norm_rotate_heads(const prq_rope *r, const int32_t *positions, int M, const prq_heads *q, const prq_heads *k, float eps,
                                  prq_dtype dtype, prq_stream_t stream);
 

@@ -3,7 +3,9 @@
 // An item is rows of one adapter, from anywhere in a window of 4096 rows.  Few rows: one launch, in which a cluster has an item, sums its h and adds
 // h B^T.  Many rows: two launches, the first one for h, the second one streams y past it.  Items are worked out on the device, so that a
 // captured call follows its row table.  Sums are fp32; h goes into the second product as two bf16 terms (hi = bf16(h), lo = bf16(h - hi):
-// 16 bits and more of its significand), whose products with B the tensor cores sum in fp32.
+// 16 bits and more of its significand), whose products with B the tensor cores sum in fp32.  In a bf16 y the bits that are lost do not show; an
+// fp32 y is off by 3.6e-7 of its size (97 rows of K = 9728, rank 32) where a product in fp32 is by 0.9e-7: a third term, half again as many
+// products, would be the price of the rest.
 //
 // Up to rank 32 both products use mma.sync (16 x 8 x 16, bf16): they hold 16 to 64 flop per byte of y, too little for its rate to become the
 // bound.  Rows may stand in any order, and sums stay in the registers of the lane that stores them.  The order of a reduction's elements is
@@ -80,12 +82,16 @@ struct __align__(16) Item {
 constexpr int kItemsSoon = 24;        // items times passes that clusters of eight CTAs work off in two turns
 // All ranks of all parts are summed in passes of up to 64, which small items take one after another and large ones at the same time.
 int passes_of(int n_parts, int max_rank) { return (n_parts * ((max_rank + 15) & ~15) + 63) / 64; }
-// Small items and one launch, or large ones and two.  One pass: small up to 512 rows (o of 387 rows, rank 32: 10.1 us, with large items 12.0;
-// gate / up of 512 rows, rank 16: 21 and 20; of 768: 28 and 21), and wherever adapters may have fewer rows than such an item (q / k / v, rank 16, 1000
-// rows of a pool of 64: all of them in use 23 and 80, four in use 23 and 18; of a pool of 500 102 and 582, 23 and 18).  Several passes: large where
-// there cannot be more items than clusters work off soon (q / k / v, rank 64, one row: 9.1 and 17 with a small item; 48 rows of a pool of 4: 10 to 12
-// and 21; of 8: 11 to 21 and 21), small where adapters may have few rows (200 rows of a pool of 64: all in use 46 and 130, four in use 38 and 14;
-// 256 of a pool of 32: 36 and 71, 36 and 16).  And small where rows are put in order 32 at a time.
+// Small items and one launch, or large ones and two: a rule on what the host knows, which is the pool's size and not what a batch uses of it.
+// One pass: small up to 512 rows (o of 387 rows, rank 32: 10.1 us, with large items 12.0; gate / up of 512 rows, rank 16: 21 and 20; of 768: 28
+// and 21), and wherever adapters may have fewer rows than such an item (q / k / v, rank 16, 1000 rows of a pool of 64: all of them in use 23 and 80,
+// four in use 23 and 18; of a pool of 500 102 and 582, 23 and 18).  Several passes: large where there cannot be more items than clusters
+// work off soon (q / k / v, rank 64, one row: 9.1 and 17 with a small item; 48 rows of a pool of 4: 10 to 12 and 21; of 8: 11 to 21 and 21),
+// small where adapters may have few rows (200 rows of a pool of 64: all in use 46 and 130, four in use 38 and 14; 256 of a pool of 32: 36 and 71,
+// 36 and 16).  And small where rows are put in order 32 at a time.
+// What the rule costs where a large pool has four adapters in use (q / k / v, as it is, and in a pool of four): rank 16, 200 rows of a pool of 64 to
+// 600 22 and 9 us, 1000 23 and 18, 4096 of a pool of 500 50 and 34, of 600 62; rank 64, 200 rows of a pool of 64 to 600 38 and 14, 1000 39
+// and 28, 2000 of a pool of 200 or 500 79 and 43, 4096 of a pool of 500 163 and 68, of 600 183.
 bool small_items(int M, int n_slots, int passes) {
     const long long room = static_cast<long long>(kFewRows) * n_slots;
     if (n_slots > kSortedSlots) return true;
@@ -255,8 +261,8 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 
 // ---------------------------------------------------------------- h
 // An item and 8 kRankTiles ranks at a time per cluster, whose CTAs split K.  Rows of x and of A come into a ring in shared memory, kStageK of K
-// at a time; a warp has 16 rows and one 32 of K in kWarpsK.  Few rows: what is on its way at once sets the pace (a CTA's share of K is a few
-// stages), so the pieces are long.  Row stride in the ring: 64 bytes off a multiple of 128, so that the eight lanes of a 16-byte load (two
+// at a time; a warp has 16 rows and one 32 of K in kWarpsK.  (With items of 16 rows a stage has 32s of K for eight of the 16 warps; the others' sums
+// are zeros.)  Few rows: what is on its way at once sets the pace (a CTA's share of K is a few stages), so the pieces are long.  Row stride in the ring: 64 bytes off a multiple of 128, so that the eight lanes of a 16-byte load (two
 // rows, four lanes each) meet no bank twice.
 template <int kRankTiles, int kItemRows>
 struct HShared {
@@ -530,8 +536,8 @@ __device__ __forceinline__ void copy_rows(const AdapterParams& p, const int* row
 }
 
 // Few rows: one launch.  Every CTA of an item's cluster gets all of its sums, and a share of the columns: 64 per warp, straight from memory.
-// Bound by a chain of latencies, not by bytes: one row of q / k / v, rank 16, 6.9 us (finding it 1, loads of x and A 2, exchange 1, loads of
-// B and base, products and stores 2); 64 rows with 58 adapters 15.8 us, 27 MB.  Two launches took 7.1 and 18.9.
+// Bound by a chain of latencies, not by bytes: one row of q / k / v, rank 16, 7.0 us (finding it 1, loads of x and A 2, exchange 1, loads of
+// B and base, products and stores 2); 64 rows with 58 adapters 15.3 us, 27 MB.  Two launches took 7.1 and 18.9.
 template <int kRankTiles>
 struct FewShared : HShared<kRankTiles, kFewRows> {
     uint4 h[kFewRows * PRQ_MULTI_MAX * PRQ_ADAPTER_MAX_RANK / 4];   // [rank / 4][row]
@@ -593,7 +599,7 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_few_kernel(const __grid
         }
 
         const bool mine[2] = {g < rows, 8 + g < rows};
-        // (lanes whose row does not exist repeat the item's first one up to the store)
+        // (lanes whose row does not exist load and store nothing)
         const long long row[2] = {mine[0] ? sh.row[g] : 0, mine[1] ? sh.row[8 + g] : 0};
 #pragma unroll 1
         for (int unit = cta * kHWarps + warp; unit < units && rows > 0; unit += stride) {
@@ -656,8 +662,9 @@ __global__ void __launch_bounds__(kHThreads, 1) adapters_few_kernel(const __grid
     }
 }
 
-// Many rows: a CTA has every y_items-th item of a window, and `span` tiles of kCols columns of one part.  Bound by memory: 4096 rows of
-// q / k / v in place, rank 16, 25 us for 101 MB, 4 TB/s (a copy in place of that pattern takes 20 to 22).  Tiles of base and B come into a ring in shared memory; a
+// Many rows: a CTA has every y_items-th item of a window, and `span` tiles of kCols columns of one part.  4096 rows of q / k / v in place, rank
+// 16: 25 us for 101 MB, 4 TB/s (a copy in place of that pattern takes 20 to 22).  It waits for its loads (the long scoreboard is the largest
+// stall); no pipe is more than a third busy, and HBM a quarter when the launch stands alone.  Tiles of base and B come into a ring in shared memory; a
 // warp has 16 of the item's rows, whose h it keeps in registers, and all columns.  In the ring a row of B stands where the fragment's
 // lane wants it (row n of a block of 32 at 8 ((n % 8) / 2) + 2 (n / 8) + n % 2), with a stride of 32 bytes off a multiple of 64; of base,
 // odd rows have the halves of their 128 bytes swapped: no lane of a load meets another one's bank.
@@ -815,8 +822,9 @@ __global__ void __launch_bounds__(kManyThreads, kSteps16 == 1 ? 3 : 2) adapters_
 // row, which neighbouring threads copy, stay within 128 bytes.  (Without swizzle each goes to a line of shared memory of its own, and
 // the copies of one tile of B took 2500 cycles instead of 300.)  Rows of base: piece i of row r (16 bytes) at
 // i ^ (r & 7), so that eight threads with a row each meet no bank twice.
-// Bound by shared memory, which a tile passes five times (base and B in, operands, base again, and out): 4096 rows of gate / up in place, rank
-// 64, 87 us for 319 MB, 3.7 TB/s; with fragments from shared memory (mma.sync) 110.
+// 4096 rows of gate / up in place, rank 64: 88 us for 319 MB, 3.6 TB/s; with fragments from shared memory (mma.sync) 110.  It waits: all warps of
+// the SM's only CTA are in the same phase (tensor core, tile out, stores, loads of the tile after the next one), and one tile of loads is on its
+// way meanwhile.  The long scoreboard is the largest stall; HBM is 44 % busy, the load and store pipe 31 %, issue 36 %.
 constexpr int kHighThreads = 512, kHighWarps = kHighThreads / 32;
 constexpr int kKBytes = 128;      // of K per row of an operand's block
 struct HighShared { int blocks, h, base, b, total; };   // blocks of K; bytes of h, a tile of base, of B, and in all, with two of each tile
@@ -1222,7 +1230,7 @@ cudaError_t launch_many_h(const AdapterParams& p, cudaStream_t stream) {
 template <class T>
 cudaError_t launch_many_y(AdapterParams p, int num_sms, cudaStream_t stream) {
     // Tensor memory for ranks above 32 where a CTA has many tiles (gate / up of 4096 tokens, 16 tiles of 256 columns per SM: rank 64 125 us
-    // with mma.sync, 105 so; rank 32 84 and 98; q / k / v, five per SM: rank 64 68 either way, rank 32 42 and 54; 1024 tokens of gate / up,
+    // with mma.sync, 109 to 111 so; rank 32 84 and 98; q / k / v, five per SM: rank 64 68 either way, rank 32 42 and 54; 1024 tokens of gate / up,
     // rank 64: 47 either way), and for ranks above 64, whose h mma.sync's registers do not hold.
     const int items = (p.M + kManyRows - 1) / kManyRows;
     if (p.pad_rank > 64) return launch_high_y<T, 256>(p, num_sms, stream);
