@@ -4,7 +4,7 @@
 // h B^T.  Many rows: two launches, the first one for h, the second one streams y past it.  Items are worked out on the device, so that a
 // captured call follows its row table.  Sums are fp32; h goes into the second product as two bf16 terms (hi = bf16(h), lo = bf16(h - hi):
 // 16 bits and more of its significand), whose products with B the tensor cores sum in fp32.  In a bf16 y the bits that are lost do not show; an
-// fp32 y is off by 3.6e-7 of its size (97 rows of K = 9728, rank 32) where a product in fp32 is by 0.9e-7: a third term, half again as many
+// fp32 y is off by 3.1 to 3.6e-7 of its size (97 rows of K = 9728, rank 32) where a product in fp32 is by 0.7 to 0.9e-7: a third term, half again as many
 // products, would be the price of the rest.
 //
 // Up to rank 32 both products use mma.sync (16 x 8 x 16, bf16): they hold 16 to 64 flop per byte of y, too little for its rate to become the
